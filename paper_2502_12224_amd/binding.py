@@ -29,6 +29,8 @@ EXPORTS = [
     "fate_hip_engine_copy", "fate_hip_engine_begin_step", "fate_hip_engine_wait_ready",
     "fate_hip_engine_preload", "fate_hip_engine_bytes_copied",
     "fate_eap_create", "fate_eap_destroy", "fate_eap_update", "fate_eap_predict",
+    "fate_mx_quantize", "fate_mx_weight_bytes", "fate_mx_pack_weight", "fate_add_rmsnorm", "fate_mx_linear",
+    "fate_moe_ffn_mx_workspace", "fate_moe_ffn_mx",
 ]
 
 
@@ -119,6 +121,13 @@ def lib():
         L.fate_eap_destroy.argtypes = [C.c_void_p]
         L.fate_eap_update.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int]
         L.fate_eap_predict.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p]
+        P, I, I64 = C.c_void_p, C.c_int, C.c_int64
+        L.fate_mx_quantize.argtypes = [P, P, I, I, I, I64, P, P]
+        L.fate_mx_weight_bytes.argtypes = [I, I, I, P, P]
+        L.fate_mx_pack_weight.argtypes = [P, P, I, I, I, I64, I, P, P]
+        L.fate_add_rmsnorm.argtypes = [P, I, I, P, I, I64, P, I, I64, P, I, C.c_float, P, I64, P, I64, P, P]
+        L.fate_mx_linear.argtypes = [P, I, I, I, P, I, I64, P, I, P, P, P, P, I, I64]
+        L.fate_moe_ffn_mx.argtypes = [P] * 15 + [C.c_size_t]
         _lib = L
     return _lib
 
@@ -306,3 +315,187 @@ def make_ffn_desc(N, H, E, k, I_max, bits, group, n_shared=0, I_shared_max=0, sh
                   y_is_fp32=True, mode=0):
     return fate_ffn_desc(N, H, E, k, I_max, bits, group, n_shared, I_shared_max, shared_bits, shared_group,
                          int(y_is_fp32), mode, 0)
+
+
+# ---------------------------------------------------------------------------
+# block-scaled 8- and 4-bit values
+# ---------------------------------------------------------------------------
+
+FATE_BF16, FATE_FP32, FATE_MXFP8 = 0, 1, 2
+_TYPE_OF = {torch.bfloat16: FATE_BF16, torch.float32: FATE_FP32}
+MX_GROUP = 32
+
+
+def _need(cond, msg):
+    if not cond:
+        raise FateError(1, msg)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows(t, name, shape=None):
+    """(type, distance between rows) of a matrix whose rows are contiguous."""
+    _need(t.dim() == 2 and t.dtype in _TYPE_OF, f"{name} is a matrix of bf16 or fp32")
+    _need(shape is None or t.shape == shape, f"{name} is {tuple(t.shape)}, {tuple(shape or ())} expected")
+    _need(t.stride(1) == 1 or t.shape[1] == 1, f"the rows of {name} are not contiguous")
+    # (a single row has no distance, whatever its stride says)
+    return _TYPE_OF[t.dtype], max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _dense(t, name, dtype, shape):
+    _need(t.dtype == dtype and t.shape == shape and t.is_contiguous(), f"{name} is a contiguous {dtype} tensor {tuple(shape)}")
+
+
+def _here(stream, *tensors):
+    """The stream to launch on: tensors of a launch live on the current device, which owns the stream."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise FateError(1, f"a tensor on {t.device}, the current device is cuda:{dev}")
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _apart(out, *inputs):
+    """Outputs that are their own memory: a full overlap with an input is always a mistake."""
+    for t in inputs:
+        _need(t is None or out is None or out.data_ptr() != t.data_ptr() or out.numel() == 0, "an output is also an input")
+
+
+def mx_padded(K):
+    """Columns of 8-bit rows: K rounded up to a multiple of 128."""
+    return -(-K // 128) * 128
+
+
+def mx_empty(rows, K, device="cuda"):
+    """Room for 8-bit rows: (codes [rows, Kp], scales [rows, Kp / 32])."""
+    Kp = mx_padded(K)
+    return (torch.empty(rows, Kp, dtype=torch.uint8, device=device),
+            torch.empty(rows, Kp // MX_GROUP, dtype=torch.uint8, device=device))
+
+
+def _check_mx(codes, scales, rows, K, name):
+    Kp = mx_padded(K)
+    _dense(codes, f"{name} codes", torch.uint8, (rows, Kp))
+    _dense(scales, f"{name} scales", torch.uint8, (rows, Kp // MX_GROUP))
+
+
+def fate_mx_quantize(x, codes, scales, stream=None):
+    t, ld = _rows(x, "x")
+    N, K = x.shape
+    _check_mx(codes, scales, N, K, "output")
+    _check(lib().fate_mx_quantize(_here(stream, x, codes, scales), x.data_ptr(), t, N, K, ld, codes.data_ptr(),
+                                  scales.data_ptr()))
+
+
+def fate_mx_weight_bytes(rows, K, bits):
+    """(bytes of the codes, bytes of the scales) of a packed matrix."""
+    c, s = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().fate_mx_weight_bytes(rows, K, bits, C.byref(c), C.byref(s)))
+    return c.value, s.value
+
+
+def fate_mx_pack_weight(w, bits, codes, scales, stream=None):
+    t, ld = _rows(w, "w")
+    cb, sb = fate_mx_weight_bytes(*w.shape, bits)
+    _dense(codes, "codes", torch.uint8, (cb,))
+    _dense(scales, "scales", torch.uint8, (sb,))
+    _check(lib().fate_mx_pack_weight(_here(stream, w, codes, scales), w.data_ptr(), t, *w.shape, ld, bits,
+                                     codes.data_ptr(), scales.data_ptr()))
+
+
+class MxWeight:
+    """Device-native copy of one matrix [R, K] (bf16 or fp32 on the device) in 4 or 8 bits."""
+
+    def __init__(self, w, bits, stream=None):
+        self.R, self.K = w.shape
+        self.bits = bits
+        cb, sb = fate_mx_weight_bytes(self.R, self.K, bits)
+        self.codes = torch.empty(cb, dtype=torch.uint8, device=w.device)
+        self.scales = torch.empty(sb, dtype=torch.uint8, device=w.device)
+        fate_mx_pack_weight(w, bits, self.codes, self.scales, stream)
+
+    def nbytes(self):
+        return self.codes.numel() + self.scales.numel()
+
+
+class MxExpert:
+    """One SwiGLU expert of block-scaled matrices W1 [I, H], W3 [I, H], W2 [H, I]."""
+
+    def __init__(self, w1, w3, w2):
+        _need(w1.bits == w3.bits == w2.bits and (w1.R, w1.K) == (w3.R, w3.K) == (w2.K, w2.R), "W1, W3 and W2 do not fit")
+        self.w1, self.w3, self.w2, self.bits, self.group, self.I, self.H = w1, w3, w2, w1.bits, MX_GROUP, w1.R, w1.K
+
+    def struct(self):
+        w = (self.w1, self.w3, self.w2)
+        return fate_qexpert(*[m.codes.data_ptr() for m in w], *[m.scales.data_ptr() for m in w], self.bits, self.group,
+                            self.I, 0, None, None, None, 0)
+
+    def nbytes(self):
+        return self.w1.nbytes() + self.w3.nbytes() + self.w2.nbytes()
+
+
+def fate_add_rmsnorm(h, delta=None, weight=None, eps=1e-6, h_out=None, x=None, mx=None, stream=None):
+    """h [N, H], delta [N, H] or None, weight [H] or None; outputs h_out [N, H] of h's type (may be h), x [N, H] bf16,
+    mx = (codes, scales), each of them or None."""
+    N, H = h.shape
+    th, ld_h = _rows(h, "h")
+    td = ld_d = tw = ld_o = ld_x = 0
+    if delta is not None:
+        td, ld_d = _rows(delta, "delta", h.shape)
+    if weight is not None:
+        _need(weight.dtype in _TYPE_OF and weight.shape == (H,) and weight.is_contiguous(), "weight is a vector [H] of bf16 or fp32")
+        tw = _TYPE_OF[weight.dtype]
+    if h_out is not None:
+        to, ld_o = _rows(h_out, "h_out", h.shape)
+        _need(to == th, "h_out has h's type")
+        _apart(h_out, delta, weight)
+    if x is not None:
+        tx, ld_x = _rows(x, "x", h.shape)
+        _need(tx == FATE_BF16, "x is bf16")
+        _apart(x, h, delta, weight, h_out)
+    codes = scales = None
+    if mx is not None:
+        codes, scales = mx
+        _check_mx(codes, scales, N, H, "x")
+    _check(lib().fate_add_rmsnorm(_here(stream, h, delta, weight, h_out, x, codes, scales), N, H, h.data_ptr(), th, ld_h,
+                                  _ptr(delta), td, ld_d, _ptr(weight), tw, eps, _ptr(h_out), ld_o, _ptr(x), ld_x,
+                                  _ptr(codes), _ptr(scales)))
+
+
+def fate_mx_linear(x, w, y, bias=None, stream=None):
+    """x: a bf16 matrix [N, K], or 8-bit rows (codes, scales); w: an MxWeight [R, K]; y [N, R] bf16 or fp32."""
+    if isinstance(x, tuple):
+        x, xs = x
+        N, tx, ld_x = x.shape[0], FATE_MXFP8, 0
+        _check_mx(x, xs, N, w.K, "x")
+    else:
+        xs, N = None, x.shape[0]
+        tx, ld_x = _rows(x, "x", (N, w.K))
+        _need(tx == FATE_BF16, "x is bf16 or 8-bit rows")
+    ty, ld_y = _rows(y, "y", (N, w.R))
+    if bias is not None:
+        _dense(bias, "bias", torch.float32, (w.R,))
+    _apart(y, x, bias)
+    _check(lib().fate_mx_linear(_here(stream, x, xs, w.codes, w.scales, bias, y), N, w.K, w.R, x.data_ptr(), tx, ld_x,
+                                _ptr(xs), w.bits, w.codes.data_ptr(), w.scales.data_ptr(), _ptr(bias), y.data_ptr(), ty,
+                                ld_y))
+
+
+def fate_moe_ffn_mx_workspace(desc):
+    b = C.c_size_t(0)
+    _check(lib().fate_moe_ffn_mx_workspace(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def fate_moe_ffn_mx(desc, x_codes, x_scales, experts_dev, counts, offsets, perm, inv_perm, expert_order, topk_w,
+                    shared_dev, shared_gate, y, workspace, stream=None):
+    _check_mx(x_codes, x_scales, desc.N, desc.H, "x")
+    _dense(y, "y", torch.float32 if desc.y_is_fp32 else torch.bfloat16, (desc.N, desc.H))
+    _check(lib().fate_moe_ffn_mx(_here(stream, x_codes, x_scales, experts_dev, counts, offsets, perm, inv_perm,
+                                       expert_order, topk_w, shared_dev, shared_gate, y, workspace), C.addressof(desc),
+                                 x_codes.data_ptr(), x_scales.data_ptr(), _ptr(experts_dev), _ptr(counts), _ptr(offsets),
+                                 _ptr(perm), _ptr(inv_perm), _ptr(expert_order), _ptr(topk_w), _ptr(shared_dev),
+                                 _ptr(shared_gate), y.data_ptr(), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size()))

@@ -1,0 +1,123 @@
+// Block-scaled 8- and 4-bit values: sizes of the layouts and the quantisers (see include/fate.h for the format).
+//
+// Device-native weights: tiles of 16 rows x 128 columns, tile (rb, kt) at rb * KT + kt, rows padded to 32.  A tile is
+// what one v_mfma_scale_f32_16x16x128_f8f6f4 takes, a wave's load one contiguous KiB:
+//   4 bits: lane l holds row l % 16, columns 32 (l / 16) .. + 31, the even column in the low nibble (16 bytes a lane);
+//   8 bits: two KiB, half h: lane l holds row l % 16, columns 64 h + 16 (l / 16) .. + 15.
+// (That is the operand layout of the instruction, found with single non-zero codes: 8-bit operands split their 32
+// columns per lane in two pieces 64 apart, 4-bit ones do not, while the scale of lane l belongs to row l % 16, columns
+// 32 (l / 16) .. + 31 in both.)
+// Scales: byte j of dword ((rb * KG + kg) * 64 + l) is the scale of lane l in tile column kt = 4 kg + j, so one dword a
+// lane serves four tiles, the instruction picks the byte.
+#pragma once
+#include "common.h"
+
+namespace fate {
+
+constexpr int kMxBlock = 32, kMxStep = 128;
+
+__host__ __device__ inline int mx_steps(int K) { return (K + kMxStep - 1) / kMxStep; }                  // KT
+__host__ __device__ inline int mx_step_groups(int K) { return (mx_steps(K) + 3) / 4; }                  // KG
+__host__ __device__ inline int mx_padded(int K) { return mx_steps(K) * kMxStep; }                       // Kp
+__host__ __device__ inline int mx_row_tiles(int rows) { return (rows + 31) / 32 * 2; }
+__host__ __device__ inline long long mx_codes_bytes(int rows, int K, int bits) {
+    return (long long)mx_row_tiles(rows) * mx_steps(K) * (bits == 4 ? 1024 : 2048);
+}
+__host__ __device__ inline long long mx_scales_bytes(int rows, int K) {
+    return (long long)mx_row_tiles(rows) * mx_step_groups(K) * 256;
+}
+
+#ifdef __HIPCC__
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// Bits of |v|: they order like the values, and NaN and infinity come out on top.
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Scale byte of a block from the largest |v|'s bits: with |v| = 1.m 2^E the smallest 2^e with |v| / 2^e <= 1.75 2^8
+// (448) is e = E - 8 + (1.m > 1.75), for 1.5 2^2 (6) it is E - 2 + (1.m > 1.5); 255 if the block is not finite.
+template <int BITS>
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax) {
+    const int E = (int)(amax >> 23);
+    if (E == 255) return 255u;
+    const int lead = BITS == 8 ? 8 : 2;
+    const uint32_t top = BITS == 8 ? 0x600000u : 0x400000u;
+    const int b = E - lead + ((amax & 0x7fffffu) > top ? 1 : 0);
+    return (uint32_t)(b > 0 ? b : 0);
+}
+// 2^(127 - b) for b <= 254 - 2 + 1; a power of two, so multiplying by it rounds nothing that matters.
+__device__ __forceinline__ float mx_inverse_scale(uint32_t b) { return __uint_as_float((254u - (b > 253u ? 253u : b)) << 23); }
+
+// Four values over their scale -> four E4M3 codes (the conversion rounds to nearest, ties to even).
+__device__ __forceinline__ uint32_t mx_codes8(float a, float b, float c, float d, uint32_t scale) {
+    const float inv = mx_inverse_scale(scale);
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, r, true);
+    return scale == 255u ? 0x7f7f7f7fu : (uint32_t)r;
+}
+// One value over its scale -> E2M1 code, to nearest, ties to the even code.
+__device__ __forceinline__ uint32_t mx_code4(float v, uint32_t scale) {
+    const float a = fabsf(v) * mx_inverse_scale(scale);
+    const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
+    return scale == 255u ? 0u : c | (v < 0.0f ? 8u : 0u);
+}
+
+// Largest bits over the four lanes of a quad.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false);   // [1,0,3,2]
+    v = v > o ? v : o;
+    o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false);            // [2,3,0,1]
+    return v > o ? v : o;
+}
+
+// Eight consecutive elements, of which the first `n` exist.  VEC: all eight exist and lie on a 16-byte boundary.
+template <bool VEC>
+__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
+    if constexpr (VEC) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p);
+        v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
+        v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_bits_to_f32(p[i]) : 0.0f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+    if constexpr (VEC) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    return f32_to_bf16_bits(a) | (f32_to_bf16_bits(b) << 16);
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]),
+                                                  bf16_pair(v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (uint16_t)f32_to_bf16_bits(v[i]);
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+    if constexpr (VEC) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+#endif
+
+}  // namespace fate

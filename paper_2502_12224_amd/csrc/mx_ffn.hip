@@ -1,0 +1,225 @@
+// fate_mx_linear and fate_moe_ffn_mx: argument checks, workspace, choice of kernels, the sum over a token's experts.
+#include "mx_gemm.h"
+
+namespace fate {
+
+int mx_stream_rows(long long rows, int Kp);
+fate_status launch_mx_stream(hipStream_t st, const MxArgs& a, bool up, int rows_cap);
+fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up, long long rows);
+fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x, const MxMatrix& m, const float* bias,
+                                  void* y, long long ld_y, int N, int K, int R, int y_fp32, int y_vec);
+
+struct MxCombineArgs {
+    const void* rows_r; const void* rows_s;
+    const int32_t* inv_perm; const float* topk_w;
+    const uint8_t* x; const uint8_t* xs; const uint16_t* gate;
+    void* y;
+    int N, k, H, n_shared, Kp;
+};
+
+template <typename T>
+__device__ __forceinline__ v4f row4(const void* rows, long long at) {
+    if constexpr (sizeof(T) == 4) return reinterpret_cast<const v4f*>(static_cast<const float*>(rows) + at)[0];
+    else {
+        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(rows) + at);
+        return v4f{bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y)};
+    }
+}
+
+// y[t] = sum_j w[t,j] row[inv_perm[t,j]] + g(t) sum_v shared row: one workgroup per token, terms in the order of j, then v.
+template <typename T>
+__global__ __launch_bounds__(256) void mx_combine_kernel(MxCombineArgs a) {
+    __shared__ float part[4];
+    const long long t = blockIdx.x;
+    float gate = 1.0f;
+    if (a.gate != nullptr) {
+        float s = 0.0f;
+        for (int i = (int)threadIdx.x * 4; i < a.H; i += 1024) {
+            const int c = *reinterpret_cast<const int*>(a.x + t * a.Kp + i);
+            const uint32_t b = a.xs[(t * a.Kp + i) / kMxBlock];
+            const float f = b == 255u ? __builtin_nanf("") : __uint_as_float(b ? b << 23 : 0x400000u);
+            const uint2 w = *reinterpret_cast<const uint2*>(a.gate + i);
+            s += f * (__builtin_amdgcn_cvt_f32_fp8(c, 0) * bf16_lo(w.x) + __builtin_amdgcn_cvt_f32_fp8(c, 1) * bf16_hi(w.x) +
+                      __builtin_amdgcn_cvt_f32_fp8(c, 2) * bf16_lo(w.y) + __builtin_amdgcn_cvt_f32_fp8(c, 3) * bf16_hi(w.y));
+        }
+        s = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+        __syncthreads();
+        gate = 1.0f / (1.0f + __expf(-((part[0] + part[1]) + (part[2] + part[3]))));
+    }
+    const int P = a.N * a.k;
+    for (int i = (int)threadIdx.x * 4; i < a.H; i += 1024) {
+        v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int j = 0; j < a.k; ++j) {
+            const int s = a.inv_perm[t * a.k + j];
+            const float w = a.topk_w[t * a.k + j];
+            if ((unsigned)s < (unsigned)P) y += w * row4<T>(a.rows_r, (long long)s * a.H + i);
+        }
+        v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int v = 0; v < a.n_shared; ++v) z += row4<T>(a.rows_s, ((long long)v * a.N + t) * a.H + i);
+        y += gate * z;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f*>(static_cast<float*>(a.y) + t * a.H + i) = y;
+        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.H + i) =
+                 make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+    }
+}
+
+static fate_status check_mx_desc(const fate_ffn_desc* d) {
+    if (d == nullptr) FATE_FAIL(FATE_EINVAL, "descriptor is NULL");
+    if (d->N < 0) FATE_FAIL(FATE_EINVAL, "N = %d < 0", d->N);
+    if (d->E < 1 || d->E > kMaxE) FATE_FAIL(FATE_ESHAPE, "E = %d outside [1, %d]", d->E, kMaxE);
+    if (d->k < 1 || d->k > d->E || d->k > kMaxM) FATE_FAIL(FATE_EINVAL, "k = %d outside [1, min(E, %d)]", d->k, kMaxM);
+    if (d->H < 32 || d->H % 32 || d->H > (1 << 20)) FATE_FAIL(FATE_ESHAPE, "H = %d must be a multiple of 32 up to 2^20", d->H);
+    if (d->I_max < 32 || d->I_max % 32 || d->I_max > (1 << 20)) FATE_FAIL(FATE_ESHAPE, "I_max = %d must be a multiple of 32 up to 2^20", d->I_max);
+    if (d->bits != 4 && d->bits != 8) FATE_FAIL(FATE_EINVAL, "bits = %d (4 or 8)", d->bits);
+    if (d->group != kMxBlock) FATE_FAIL(FATE_ESHAPE, "group = %d (blocks are of %d)", d->group, kMxBlock);
+    if (d->n_shared < 0 || d->n_shared > 16) FATE_FAIL(FATE_EINVAL, "n_shared = %d outside [0, 16]", d->n_shared);
+    if (d->n_shared) {
+        if (d->shared_bits != 4 && d->shared_bits != 8) FATE_FAIL(FATE_EINVAL, "shared_bits = %d (4 or 8)", d->shared_bits);
+        if (d->shared_group != kMxBlock) FATE_FAIL(FATE_ESHAPE, "shared_group = %d (blocks are of %d)", d->shared_group, kMxBlock);
+        if (d->I_shared_max < 32 || d->I_shared_max % 32 || d->I_shared_max > (1 << 20))
+            FATE_FAIL(FATE_ESHAPE, "I_shared_max = %d must be a multiple of 32 up to 2^20", d->I_shared_max);
+    }
+    if (d->mode != 0) FATE_FAIL(FATE_EINVAL, "mode = %d (0 only)", d->mode);
+    if (d->reserved != 0) FATE_FAIL(FATE_EINVAL, "the descriptor's reserved field must be 0");
+    if ((long long)d->N * d->k > 0x3fffffffLL || (long long)d->N * (d->n_shared ? d->n_shared : 1) > 0x3fffffffLL)
+        FATE_FAIL(FATE_ESHAPE, "N*k too large");
+    return FATE_OK;
+}
+
+struct MxWorkspace {
+    size_t h_r, hs_r, h_s, hs_s, rows_r, rows_s, bytes;
+};
+
+static MxWorkspace mx_workspace(const fate_ffn_desc& d) {
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    MxWorkspace w;
+    const size_t P = (size_t)d.N * d.k, S = (size_t)d.N * d.n_shared;
+    const size_t Ip = mx_padded(d.I_max), Is = d.n_shared ? mx_padded(d.I_shared_max) : 0;
+    size_t off = 256;                                             // status word
+    w.h_r = off; off += up(P * Ip);
+    w.hs_r = off; off += up(P * Ip / kMxBlock);
+    w.h_s = off; off += up(S * Is);
+    w.hs_s = off; off += up(S * Is / kMxBlock);
+    w.rows_r = off; off += up(P * d.H * (d.y_is_fp32 ? 4 : 2));
+    w.rows_s = off; off += up(S * d.H * (d.y_is_fp32 ? 4 : 2));
+    w.bytes = off;
+    return w;
+}
+
+// Few rows per group, and they fit into LDS: weights are streamed once for 16 rows each; otherwise tiles.
+static fate_status launch_product(hipStream_t st, const MxArgs& a, bool up) {
+    const long long P = (long long)a.N * a.k;
+    const long long cap_rows = a.E && P > a.N ? P : a.N;
+    const int Kp = a.Kp_r > a.Kp_s ? a.Kp_r : a.Kp_s;
+    const int cap = mx_stream_rows(cap_rows, Kp);
+    const long long groups = a.E ? (P < a.E ? P : a.E) : 1;
+    const long long rows = a.E ? (P + groups - 1) / groups : a.N;
+    if (cap && a.N <= 16) return launch_mx_stream(st, a, up, cap);
+    return launch_mx_tile(st, a, up, rows);
+}
+
+}  // namespace fate
+
+using namespace fate;
+
+extern "C" fate_status fate_mx_linear(void* stream, int N, int K, int R, const void* x, int x_type, int64_t ld_x,
+                                      const void* x_scales, int bits, const void* w_codes, const void* w_scales,
+                                      const float* bias, void* y, int y_type, int64_t ld_y) {
+    if (N < 0) FATE_FAIL(FATE_EINVAL, "N = %d < 0", N);
+    if (K < 1 || K > (1 << 24) || R < 1 || R > (1 << 24))
+        FATE_FAIL(FATE_ESHAPE, "K = %d, R = %d (1 to 2^24 each)", K, R);
+    if (bits != 4 && bits != 8) FATE_FAIL(FATE_EINVAL, "bits = %d (4 or 8)", bits);
+    if (x_type != FATE_BF16 && x_type != FATE_MXFP8) FATE_FAIL(FATE_EINVAL, "x_type = %d (FATE_BF16 or FATE_MXFP8)", x_type);
+    if (y_type != FATE_BF16 && y_type != FATE_FP32) FATE_FAIL(FATE_EINVAL, "y_type = %d (FATE_BF16 or FATE_FP32)", y_type);
+    if (x_type == FATE_BF16 && ld_x < K) FATE_FAIL(FATE_ESHAPE, "rows of x lie at least K = %d elements apart", K);
+    if (x_type == FATE_BF16 && K > 65536) FATE_FAIL(FATE_ESHAPE, "K = %d > 65536 with bf16 rows", K);
+    if (x_type == FATE_BF16 && x_scales) FATE_FAIL(FATE_EINVAL, "bf16 rows have no x_scales");
+    if (ld_y < R) FATE_FAIL(FATE_ESHAPE, "rows of y lie at least R = %d elements apart", R);
+    if (N == 0) return FATE_OK;
+    FATE_CHECK_PTR(x);
+    if (x_type == FATE_MXFP8) FATE_CHECK_PTR(x_scales);
+    FATE_CHECK_PTR(w_codes);
+    FATE_CHECK_PTR(w_scales);
+    FATE_CHECK_PTR_OPT(bias);
+    FATE_CHECK_PTR(y);
+    MxMatrix m{static_cast<const uint8_t*>(w_codes), static_cast<const uint8_t*>(w_scales), nullptr, nullptr, bits,
+               mx_steps(K), mx_step_groups(K), R};
+    const int y_fp32 = y_type == FATE_FP32, y_vec = ld_y % 4 == 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (x_type == FATE_BF16) return launch_mx_linear_bf16(st, x, ld_x, m, bias, y, ld_y, N, K, R, y_fp32, y_vec);
+    MxArgs a{};
+    a.direct = m;
+    a.E = 0; a.n_shared = 1; a.N = N; a.k = 1;
+    a.x_s = static_cast<const uint8_t*>(x); a.xs_s = static_cast<const uint8_t*>(x_scales); a.Kp_s = mx_padded(K);
+    a.y_s = y; a.ld_s = ld_y; a.cols_s = R; a.K_s = K;
+    a.down = 1; a.y_fp32 = y_fp32; a.y_vec = y_vec; a.bias = bias;
+    return launch_product(st, a, false);
+}
+
+extern "C" fate_status fate_moe_ffn_mx_workspace(const fate_ffn_desc* d, size_t* bytes) {
+    const fate_status s = check_mx_desc(d);
+    if (s != FATE_OK) return s;
+    if (bytes == nullptr) FATE_FAIL(FATE_EINVAL, "bytes is NULL");
+    *bytes = mx_workspace(*d).bytes;
+    return FATE_OK;
+}
+
+extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, const void* x_codes, const void* x_scales,
+                                       const fate_qexpert* experts_dev, const int32_t* counts, const int32_t* offsets,
+                                       const int32_t* perm, const int32_t* inv_perm, const int32_t* expert_order,
+                                       const float* topk_w, const fate_qexpert* shared_dev, const void* shared_gate_bf16,
+                                       void* y, void* workspace, size_t workspace_bytes) {
+    fate_status s = check_mx_desc(d);
+    if (s != FATE_OK) return s;
+    if (d->N == 0) return FATE_OK;
+    FATE_CHECK_PTR(x_codes);
+    FATE_CHECK_PTR(x_scales);
+    FATE_CHECK_PTR(y);
+    FATE_CHECK_PTR_OPT(shared_gate_bf16);
+    if (!experts_dev || !counts || !offsets || !perm || !inv_perm || !expert_order || !topk_w)
+        FATE_FAIL(FATE_EINVAL, "experts, counts, offsets, perm, inv_perm, expert_order and topk_w must not be NULL");
+    if (d->n_shared && !shared_dev) FATE_FAIL(FATE_EINVAL, "shared_dev is NULL with n_shared = %d", d->n_shared);
+    const MxWorkspace w = mx_workspace(*d);
+    if (workspace == nullptr || workspace_bytes < w.bytes)
+        FATE_FAIL(FATE_EWORKSPACE, "workspace of %zu bytes needed, %zu given", w.bytes, workspace_bytes);
+    FATE_CHECK_PTR(workspace);
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+
+    MxArgs a{};
+    a.experts = experts_dev; a.shared = shared_dev;
+    a.offsets = offsets; a.perm = perm;
+    a.E = d->E; a.n_shared = d->n_shared; a.N = d->N; a.k = d->k;
+    a.status = reinterpret_cast<int32_t*>(base);
+    a.gather = 1;
+    a.x_r = a.x_s = static_cast<const uint8_t*>(x_codes);
+    a.xs_r = a.xs_s = static_cast<const uint8_t*>(x_scales);
+    a.Kp_r = a.Kp_s = mx_padded(d->H);
+    a.K_r = a.K_s = d->H;
+    a.y_r = base + w.h_r; a.ys_r = base + w.hs_r; a.ld_r = mx_padded(d->I_max); a.cols_r = (int)a.ld_r;
+    a.y_s = base + w.h_s; a.ys_s = base + w.hs_s;
+    a.ld_s = d->n_shared ? mx_padded(d->I_shared_max) : 0; a.cols_s = (int)a.ld_s;
+    s = launch_product(st, a, true);
+    if (s != FATE_OK) return s;
+
+    a.gather = 0;
+    a.down = 1;
+    a.x_r = base + w.h_r; a.xs_r = base + w.hs_r; a.Kp_r = mx_padded(d->I_max); a.K_r = d->I_max;
+    a.x_s = base + w.h_s; a.xs_s = base + w.hs_s;
+    a.Kp_s = d->n_shared ? mx_padded(d->I_shared_max) : 0; a.K_s = d->I_shared_max;
+    a.y_r = base + w.rows_r; a.y_s = base + w.rows_s;
+    a.ld_r = a.ld_s = a.cols_r = a.cols_s = d->H;
+    a.y_fp32 = d->y_is_fp32; a.y_vec = 1;
+    s = launch_product(st, a, false);
+    if (s != FATE_OK) return s;
+
+    MxCombineArgs c{base + w.rows_r, base + w.rows_s, inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
+                    static_cast<const uint8_t*>(x_scales), d->n_shared ? static_cast<const uint16_t*>(shared_gate_bf16) : nullptr,
+                    y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H)};
+    if (d->y_is_fp32) mx_combine_kernel<float><<<d->N, 256, 0, st>>>(c);
+    else mx_combine_kernel<uint16_t><<<d->N, 256, 0, st>>>(c);
+    FATE_HIP(hipGetLastError());
+    return FATE_OK;
+}

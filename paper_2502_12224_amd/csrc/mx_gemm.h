@@ -1,0 +1,222 @@
+// Products with block-scaled weights: what the kernels of mx_stream.hip and mx_tile.hip share.
+#pragma once
+#include "mx.h"
+
+namespace fate {
+
+// One matrix (or the pair W1, W3) of an expert as a kernel finds it.
+struct MxMatrix {
+    const uint8_t* w; const uint8_t* s;
+    const uint8_t* w3; const uint8_t* s3;   // up product only
+    int bits, KT, KG, rows;                 // tile columns, scale dwords per tile row, output rows (padded to 32: tiles exist)
+};
+
+// A product over ragged groups of rows: E groups given by `offsets` (sorted positions) and n_shared groups of all N rows
+// each.  UP: output = 8-bit rows q(silu(x W1^T) * (x W3^T)); else rows x W^T of bf16 or fp32.
+struct MxArgs {
+    const fate_qexpert* experts; const fate_qexpert* shared;
+    MxMatrix direct;                        // used instead of the tables if direct.w is set (E = 0, n_shared = 1)
+    const int32_t* offsets; const int32_t* perm;
+    int E, n_shared, N, k;
+    // sources, 8-bit rows: routed sorted position s reads row perm[s] / k if gather, row s otherwise; shared group v
+    // reads row t if gather, row v * N + t otherwise
+    int gather;
+    const uint8_t* x_r; const uint8_t* xs_r; int Kp_r;
+    const uint8_t* x_s; const uint8_t* xs_s; int Kp_s;
+    // outputs: routed row s, shared row v * N + t; ld in elements (bytes of codes for UP)
+    void* y_r; uint8_t* ys_r; long long ld_r;
+    void* y_s; uint8_t* ys_s; long long ld_s;
+    int cols_r, cols_s;                     // output columns (UP: padded to 128)
+    int K_r, K_s;                           // nominal reduction lengths (I of an entry may be smaller)
+    int down;                               // entries' w2 with K = I; otherwise w1 (and w3) with K = H
+    int y_fp32, y_vec;                      // output type; rows allow 4-wide stores
+    const float* bias;
+    int32_t* status;
+};
+
+
+#ifdef __HIPCC__
+// The piece of work number `item`: shared groups first (their reductions are the long ones), then the experts; within
+// a group the row tiles of one column block follow each other.
+struct MxItem {
+    int group;          // expert, or E + v; -1: none
+    int col, row0, rows;
+};
+
+__device__ __forceinline__ int wave_scan_inclusive(int v) {
+    const int lane = (int)(threadIdx.x & 63);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// Every wave of a workgroup works this out for itself (no barrier); E <= 256: four experts per lane.
+// xcd: spread over eight contiguous ranges, one per die, so that the row tiles of a column block share an L2.
+template <int RT, bool XCD>
+__device__ __forceinline__ MxItem mx_find_item(const MxArgs& a, int cb_r, int cb_s, int bid) {
+    const int lane = (int)(threadIdx.x & 63);
+    const int tiles_s = (a.N + RT - 1) / RT;
+    const int n_s = a.n_shared * tiles_s * cb_s;
+    int o[5], tl[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        const int e = lane * 4 + i;
+        o[i] = a.E > 0 ? a.offsets[e < a.E ? e : a.E] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        tl[i] = (o[i + 1] - o[i] + RT - 1) / RT;
+        sum += tl[i];
+    }
+    const int incl = wave_scan_inclusive(sum);
+    const int total = n_s + __builtin_amdgcn_readlane(incl, 63) * cb_r;
+    int item = bid;
+    MxItem r{-1, 0, 0, 0};
+    if constexpr (XCD) {
+        const int per = (total + 7) / 8;
+        if ((bid >> 3) >= per) return r;
+        item = (bid & 7) * per + (bid >> 3);
+    }
+    if (item >= total) return r;
+    if (item < n_s) {
+        const int per = tiles_s * cb_s;
+        const int v = item / per, q = item - v * per;
+        r.group = a.E + v;
+        r.col = q / tiles_s;
+        r.row0 = (q - r.col * tiles_s) * RT;
+        r.rows = a.N - r.row0 < RT ? a.N - r.row0 : RT;
+        return r;
+    }
+    item -= n_s;
+    // first lane whose experts end behind the item
+    const unsigned long long past = __ballot(incl * cb_r > item);
+    const int L = __builtin_ctzll(past);
+    int rest = item - (__builtin_amdgcn_readlane(incl, L) - __builtin_amdgcn_readlane(sum, L)) * cb_r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = __builtin_amdgcn_readlane(tl[i], L);
+        if (r.group < 0) {
+            if (rest < t * cb_r) {
+                const int lo = __builtin_amdgcn_readlane(o[i], L), hi = __builtin_amdgcn_readlane(o[i + 1], L);
+                r.group = L * 4 + i;
+                r.col = rest / t;
+                const int tt = rest - r.col * t;
+                r.row0 = lo + tt * RT;
+                r.rows = hi - r.row0 < RT ? hi - r.row0 : RT;
+            } else {
+                rest -= t * cb_r;
+            }
+        }
+    }
+    return r;
+}
+
+// The matrix of an item; false (and a status bit) if the entry cannot be used.
+template <bool UP>
+__device__ __forceinline__ bool mx_matrix(const MxArgs& a, int group, MxMatrix* m) {
+    if (a.direct.w != nullptr) {
+        *m = a.direct;
+        return true;
+    }
+    const bool shared = group >= a.E;
+    const fate_qexpert& e = shared ? a.shared[group - a.E] : a.experts[group];
+    const int I_max = a.down ? (shared ? a.K_s : a.K_r) : (shared ? a.cols_s : a.cols_r);
+    int bit = 0;
+    if (e.w1 == nullptr) bit = 1;
+    else if ((e.bits != 4 && e.bits != 8) || e.group != kMxBlock || e.I < kMxBlock || e.I % kMxBlock || e.I > I_max ||
+             e.z1 != nullptr) bit = 4;
+    if (bit) {
+        if (threadIdx.x == 0) atomicOr(a.status, bit);
+        return false;
+    }
+    const int K = a.down ? e.I : (shared ? a.K_s : a.K_r);
+    m->w = static_cast<const uint8_t*>(a.down ? e.w2 : e.w1);
+    m->s = static_cast<const uint8_t*>(a.down ? e.s2 : e.s1);
+    m->w3 = static_cast<const uint8_t*>(e.w3);
+    m->s3 = static_cast<const uint8_t*>(e.s3);
+    m->bits = e.bits;
+    m->KT = mx_steps(K);
+    m->KG = mx_step_groups(K);
+    m->rows = a.down ? (shared ? a.cols_s : a.cols_r) : e.I;
+    return true;
+}
+
+// acc += A (16 weight rows x 128) * B (16 token rows x 128)^T: lane l gets token l % 16, weight rows 4 (l / 16) .. + 3.
+// SEL picks the byte of the weights' scale dword; the tokens' scale is in byte 0.
+template <int SEL>
+__device__ __forceinline__ v4f mx_mfma4(v4i w, uint32_t ws, v8i x, uint32_t xs, v4f acc) {
+    const v8i w8 = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x, acc, 4, 0, SEL, (int)ws, 0, (int)xs);
+}
+template <int SEL>
+__device__ __forceinline__ v4f mx_mfma8(v8i w, uint32_t ws, v8i x, uint32_t xs, v4f acc) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, SEL, (int)ws, 0, (int)xs);
+}
+template <int BITS> struct MxWTile;                     // a lane's part of a weight tile
+template <> struct MxWTile<4> {
+    v4i v;
+    __device__ __forceinline__ void load(const uint8_t* p, int lane) { v = reinterpret_cast<const v4i*>(p)[lane]; }
+    template <int SEL> __device__ __forceinline__ v4f mfma(uint32_t ws, v8i x, uint32_t xs, v4f acc) const {
+        return mx_mfma4<SEL>(v, ws, x, xs, acc);
+    }
+    static constexpr int kBytes = 1024;
+};
+template <> struct MxWTile<8> {
+    v8i v;
+    __device__ __forceinline__ void load(const uint8_t* p, int lane) {
+        const v4i a = reinterpret_cast<const v4i*>(p)[lane], b = reinterpret_cast<const v4i*>(p)[64 + lane];
+        v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    template <int SEL> __device__ __forceinline__ v4f mfma(uint32_t ws, v8i x, uint32_t xs, v4f acc) const {
+        return mx_mfma8<SEL>(v, ws, x, xs, acc);
+    }
+    static constexpr int kBytes = 2048;
+};
+
+__device__ __forceinline__ float mx_swiglu(float a, float b) { return a / (1.0f + __expf(-a)) * b; }
+
+// 32 neurons of 16 tokens after the up product (two tiles of 16 neurons, four per lane in each) -> codes and scale of
+// their block.  The block's values lie in the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ void mx_store_h(const v4f& h0, const v4f& h1, bool live, uint8_t* codes, uint8_t* scale) {
+    const int g = (int)(threadIdx.x & 63) >> 4;
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t b0 = abs_bits(h0[i]), b1 = abs_bits(h1[i]);
+        m = m > b0 ? m : b0;
+        m = m > b1 ? m : b1;
+    }
+    uint32_t o = (uint32_t)__shfl_xor((int)m, 16);
+    m = m > o ? m : o;
+    o = (uint32_t)__shfl_xor((int)m, 32);
+    m = m > o ? m : o;
+    const uint32_t s = mx_scale_byte<8>(m);
+    if (live) {
+        *reinterpret_cast<uint32_t*>(codes + 4 * g) = mx_codes8(h0[0], h0[1], h0[2], h0[3], s);
+        *reinterpret_cast<uint32_t*>(codes + 16 + 4 * g) = mx_codes8(h1[0], h1[1], h1[2], h1[3], s);
+        if (g == 0) *scale = (uint8_t)s;
+    }
+}
+
+// Four consecutive outputs of one row.
+__device__ __forceinline__ void mx_store_y(const MxArgs& a, void* y, long long at, int left, v4f v) {
+    if (a.y_fp32) {
+        float* p = static_cast<float*>(y) + at;
+        if (a.y_vec && left >= 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+            for (int i = 0; i < 4; ++i)
+                if (i < left) p[i] = v[i];
+    } else {
+        uint16_t* p = static_cast<uint16_t*>(y) + at;
+        if (a.y_vec && left >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        else
+            for (int i = 0; i < 4; ++i)
+                if (i < left) p[i] = (uint16_t)f32_to_bf16_bits(v[i]);
+    }
+}
+#endif
+
+}  // namespace fate

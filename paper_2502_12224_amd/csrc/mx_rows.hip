@@ -1,0 +1,296 @@
+// Row kernels on block-scaled values: the residual addition with its root-mean-square norm and 8-bit output, the
+// quantisation of rows, the packing of weights.
+#include "mx.h"
+
+namespace fate {
+
+// Eight values (a quarter of a block; the quad of lanes holds the block) -> 8 codes and, from the quad's first lane,
+// the scale.
+__device__ __forceinline__ void quantize8(const float (&v)[8], uint8_t* codes, uint8_t* scale) {
+    uint32_t m = abs_bits(v[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        const uint32_t b = abs_bits(v[i]);
+        m = m > b ? m : b;
+    }
+    const uint32_t s = mx_scale_byte<8>(quad_max(m));
+    *reinterpret_cast<uint2*>(codes) = make_uint2(mx_codes8(v[0], v[1], v[2], v[3], s), mx_codes8(v[4], v[5], v[6], v[7], s));
+    if ((threadIdx.x & 3) == 0) *scale = (uint8_t)s;
+}
+
+struct NormArgs {
+    const void* h; const void* delta; const void* weight;
+    void* h_out; uint16_t* x; uint8_t* codes; uint8_t* scales;
+    long long ld_h, ld_delta, ld_h_out, ld_x;
+    int N, H, weight_fp32;
+    float eps;
+};
+
+// One row per group of 64 * W threads, W waves (W == 1: four rows per workgroup, no barrier); a thread keeps C pieces
+// of eight elements in registers, so h and delta are read once.
+template <typename TH, typename TD, int W, int C, bool VEC>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_rmsnorm_kernel(NormArgs a) {
+    constexpr int T = 64 * W;
+    __shared__ float part[W];
+    const int row = W == 1 ? (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6) : (int)blockIdx.x;
+    const int t = W == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+    if (row >= a.N) return;                              // whole waves (W == 1); never otherwise
+    const TH* h = static_cast<const TH*>(a.h) + row * a.ld_h;
+    const TD* dl = static_cast<const TD*>(a.delta) + row * a.ld_delta;
+    const bool add = a.delta != nullptr;
+    const int Hp = mx_padded(a.H);
+    float s[C][8], d[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int i = (c * T + t) * 8;
+        const int n = a.H - i;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[c][j] = d[c][j] = 0.0f;
+        if (n > 0) {
+            load8<VEC>(h + i, n, s[c]);
+            if (add) load8<VEC>(dl + i, n, d[c]);
+        }
+    }
+    float q = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s[c][j] += d[c][j];
+            q = fmaf(s[c][j], s[c][j], q);
+        }
+    q = wave_sum(q);
+    if constexpr (W > 1) {
+        if ((t & 63) == 0) part[t >> 6] = q;
+        __syncthreads();
+        q = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) q += part[w];
+    }
+    const float r = 1.0f / sqrtf(q / (float)a.H + a.eps);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int i = (c * T + t) * 8;
+        const int n = a.H - i;
+        if (n > 0 && a.h_out != nullptr) store8<VEC>(static_cast<TH*>(a.h_out) + row * a.ld_h_out + i, n, s[c]);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = s[c][j] * r;
+        if (a.weight != nullptr && n > 0) {
+            float w[8];
+            if (a.weight_fp32) load8<VEC>(static_cast<const float*>(a.weight) + i, n, w);
+            else load8<VEC>(static_cast<const uint16_t*>(a.weight) + i, n, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] *= w[j];
+        }
+        if (n > 0 && a.x != nullptr) store8<VEC>(a.x + row * a.ld_x + i, n, x);
+        if (a.codes != nullptr && i < Hp) {
+            if (n < 8) {                                 // columns from H on are zeros, also beside a NaN
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = j < n ? x[j] : 0.0f;
+            }
+            quantize8(x, a.codes + (long long)row * Hp + i, a.scales + ((long long)row * Hp + i) / kMxBlock);
+        }
+    }
+}
+
+template <typename TS, bool VEC>
+__global__ __launch_bounds__(256) void mx_quantize_kernel(const TS* __restrict__ src, long long ld, int rows, int K,
+                                                          uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const int per_row = mx_padded(K) / 8;                // a multiple of 16: quads do not cross rows
+    const long long n = (long long)rows * per_row;
+    for (long long o = (long long)blockIdx.x * 256 + threadIdx.x; o < n; o += (long long)gridDim.x * 256) {
+        const long long row = o / per_row;
+        const int i = (int)(o - row * per_row) * 8;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        if (i < K) load8<VEC>(src + row * ld + i, K - i, v);
+        quantize8(v, codes + o * 8, scales + o / 4);
+    }
+}
+
+// One thread per block of 32 weights.
+template <typename TS>
+__global__ __launch_bounds__(256) void mx_pack_weight_kernel(const TS* __restrict__ src, long long ld, int rows, int K,
+                                                             int bits, uint8_t* __restrict__ codes,
+                                                             uint8_t* __restrict__ scales) {
+    const int KT = mx_steps(K), KG = mx_step_groups(K);
+    const long long o = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (o >= (long long)mx_row_tiles(rows) * 16 * KG * 16) return;
+    const long long row = o / (KG * 16);
+    const int blk = (int)(o - row * (KG * 16));
+    const int rb = (int)(row >> 4), r = (int)(row & 15), kt = blk >> 2, g = blk & 3;
+    float v[32];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const int k = blk * 32 + i;
+        v[i] = 0.0f;
+        if (row < rows && k < K) {
+            if constexpr (sizeof(TS) == 2) v[i] = bf16_bits_to_f32(src[row * ld + k]);
+            else v[i] = src[row * ld + k];
+        }
+        const uint32_t b = abs_bits(v[i]);
+        m = m > b ? m : b;
+    }
+    const uint32_t s = bits == 4 ? mx_scale_byte<4>(m) : mx_scale_byte<8>(m);
+    scales[(((long long)rb * KG + (kt >> 2)) * 64 + g * 16 + r) * 4 + (kt & 3)] = (uint8_t)s;
+    if (kt >= KT) return;
+    const long long tile = (long long)rb * KT + kt;
+    if (bits == 4) {
+        uint32_t c[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) c[i >> 3] |= mx_code4(v[i], s) << (4 * (i & 7));
+        reinterpret_cast<uint4*>(codes)[tile * 64 + g * 16 + r] = make_uint4(c[0], c[1], c[2], c[3]);
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            uint32_t c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b = p * 16 + i * 4;
+                c[i] = mx_codes8(v[b], v[b + 1], v[b + 2], v[b + 3], s);
+            }
+            const int chunk = g * 2 + p;                 // 16 columns each
+            reinterpret_cast<uint4*>(codes)[(tile * 2 + (chunk >> 2)) * 64 + (chunk & 3) * 16 + r] =
+                make_uint4(c[0], c[1], c[2], c[3]);
+        }
+    }
+}
+
+template <typename TH, typename TD, bool VEC>
+static void launch_norm(hipStream_t st, const NormArgs& a) {
+    const int pieces = mx_padded(a.H) / 8;
+    // From 2048 rows on there are two waves per SIMD and more without splitting a row, and a row per wave needs no
+    // barrier; with fewer rows a row's latency counts, and it is spread over as many waves as have a piece.
+#define FATE_NORM(W, C)                                                                                               \
+    add_rmsnorm_kernel<TH, TD, W, C, VEC><<<(W) == 1 ? (a.N + 3) / 4 : a.N, (W) == 1 ? 256 : 64 * (W), 0, st>>>(a)
+    if (pieces <= 64) FATE_NORM(1, 1);
+    else if (a.N >= 2048 && pieces <= 128) FATE_NORM(1, 2);
+    else if (a.N >= 2048 && pieces <= 256) FATE_NORM(1, 4);
+    else if (a.N >= 2048 && pieces <= 512) FATE_NORM(1, 8);
+    else if (pieces <= 128) FATE_NORM(2, 1);
+    else if (pieces <= 256) FATE_NORM(4, 1);
+    else if (pieces <= 512) FATE_NORM(8, 1);
+    else if (pieces <= 1024) FATE_NORM(16, 1);
+    else if (pieces <= 2048) FATE_NORM(16, 2);
+    else FATE_NORM(16, 8);
+#undef FATE_NORM
+}
+
+static bool plain_type(int t) { return t == FATE_BF16 || t == FATE_FP32; }
+// Eight elements of every row on a 16-byte boundary (base pointers are).
+static bool rows_of_16_bytes(int type, long long ld) { return ld % (type == FATE_FP32 ? 4 : 8) == 0; }
+
+}  // namespace fate
+
+using namespace fate;
+
+extern "C" fate_status fate_add_rmsnorm(void* stream, int N, int H, const void* h, int h_type, int64_t ld_h,
+                                        const void* delta, int delta_type, int64_t ld_delta, const void* weight,
+                                        int weight_type, float eps, void* h_out, int64_t ld_h_out, void* x_bf16,
+                                        int64_t ld_x, void* x_codes, void* x_scales) {
+    if (N < 0) FATE_FAIL(FATE_EINVAL, "N = %d < 0", N);
+    if (H < 1 || H > 65536) FATE_FAIL(FATE_ESHAPE, "H = %d outside [1, 65536]", H);
+    if (!plain_type(h_type) || (delta && !plain_type(delta_type)) || (weight && !plain_type(weight_type)))
+        FATE_FAIL(FATE_EINVAL, "h, delta and weight are FATE_BF16 or FATE_FP32");
+    if (!(eps >= 0.0f)) FATE_FAIL(FATE_EINVAL, "eps = %g must not be negative", (double)eps);
+    if (N == 0) return FATE_OK;                          // (tensors without elements have NULL pointers)
+    if (!h_out && !x_bf16 && !x_codes) FATE_FAIL(FATE_EINVAL, "no output");
+    if ((x_codes == nullptr) != (x_scales == nullptr)) FATE_FAIL(FATE_EINVAL, "x_codes and x_scales come together");
+    if (ld_h < H || (delta && ld_delta < H) || (h_out && ld_h_out < H) || (x_bf16 && ld_x < H))
+        FATE_FAIL(FATE_ESHAPE, "rows lie at least H = %d elements apart", H);
+    FATE_CHECK_PTR(h);
+    FATE_CHECK_PTR_OPT(delta);
+    FATE_CHECK_PTR_OPT(weight);
+    FATE_CHECK_PTR_OPT(h_out);
+    FATE_CHECK_PTR_OPT(x_bf16);
+    FATE_CHECK_PTR_OPT(x_codes);
+    FATE_CHECK_PTR_OPT(x_scales);
+    if (h_out == h && ld_h_out != ld_h) FATE_FAIL(FATE_EINVAL, "h_out is h with another distance between rows");
+    NormArgs a{h, delta, weight, h_out, static_cast<uint16_t*>(x_bf16), static_cast<uint8_t*>(x_codes),
+               static_cast<uint8_t*>(x_scales), ld_h, delta ? ld_delta : 0, ld_h_out, ld_x, N, H,
+               weight_type == FATE_FP32, eps};
+    const bool vec = H % 8 == 0 && rows_of_16_bytes(h_type, ld_h) && (!delta || rows_of_16_bytes(delta_type, ld_delta)) &&
+                     (!h_out || rows_of_16_bytes(h_type, ld_h_out)) && (!x_bf16 || rows_of_16_bytes(FATE_BF16, ld_x));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool hf = h_type == FATE_FP32, df = delta && delta_type == FATE_FP32;
+    if (vec) {
+        if (hf) df ? launch_norm<float, float, true>(st, a) : launch_norm<float, uint16_t, true>(st, a);
+        else df ? launch_norm<uint16_t, float, true>(st, a) : launch_norm<uint16_t, uint16_t, true>(st, a);
+    } else {
+        if (hf) df ? launch_norm<float, float, false>(st, a) : launch_norm<float, uint16_t, false>(st, a);
+        else df ? launch_norm<uint16_t, float, false>(st, a) : launch_norm<uint16_t, uint16_t, false>(st, a);
+    }
+    FATE_HIP(hipGetLastError());
+    return FATE_OK;
+}
+
+extern "C" fate_status fate_mx_quantize(void* stream, const void* src, int src_type, int rows, int K, int64_t ld_src,
+                                        void* codes, void* scales) {
+    if (rows < 0) FATE_FAIL(FATE_EINVAL, "rows = %d < 0", rows);
+    if (K < 1 || K > (1 << 24)) FATE_FAIL(FATE_ESHAPE, "K = %d outside [1, 2^24]", K);
+    if (!plain_type(src_type)) FATE_FAIL(FATE_EINVAL, "src_type = %d (FATE_BF16 or FATE_FP32)", src_type);
+    if (ld_src < K) FATE_FAIL(FATE_ESHAPE, "rows lie at least K = %d elements apart", K);
+    if (rows == 0) return FATE_OK;
+    FATE_CHECK_PTR(src);
+    FATE_CHECK_PTR(codes);
+    FATE_CHECK_PTR(scales);
+    const long long n = (long long)rows * (mx_padded(K) / 8);
+    const unsigned grid = (unsigned)((n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    uint8_t* c = static_cast<uint8_t*>(codes);
+    uint8_t* s = static_cast<uint8_t*>(scales);
+    const bool vec = K % 8 == 0 && rows_of_16_bytes(src_type, ld_src);
+    if (src_type == FATE_FP32) {
+        const float* p = static_cast<const float*>(src);
+        if (vec) mx_quantize_kernel<float, true><<<grid, 256, 0, st>>>(p, ld_src, rows, K, c, s);
+        else mx_quantize_kernel<float, false><<<grid, 256, 0, st>>>(p, ld_src, rows, K, c, s);
+    } else {
+        const uint16_t* p = static_cast<const uint16_t*>(src);
+        if (vec) mx_quantize_kernel<uint16_t, true><<<grid, 256, 0, st>>>(p, ld_src, rows, K, c, s);
+        else mx_quantize_kernel<uint16_t, false><<<grid, 256, 0, st>>>(p, ld_src, rows, K, c, s);
+    }
+    FATE_HIP(hipGetLastError());
+    return FATE_OK;
+}
+
+static fate_status check_weight(int rows, int K, int bits) {
+    if (bits != 4 && bits != 8) FATE_FAIL(FATE_EINVAL, "bits = %d (4 or 8)", bits);
+    if (rows < 1 || rows > (1 << 24) || K < 1 || K > (1 << 24))
+        FATE_FAIL(FATE_ESHAPE, "a matrix of %d rows and %d columns (1 to 2^24 each)", rows, K);
+    return FATE_OK;
+}
+
+extern "C" fate_status fate_mx_weight_bytes(int rows, int K, int bits, size_t* codes_bytes, size_t* scales_bytes) {
+    const fate_status s = check_weight(rows, K, bits);
+    if (s != FATE_OK) return s;
+    if (!codes_bytes || !scales_bytes) FATE_FAIL(FATE_EINVAL, "codes_bytes or scales_bytes is NULL");
+    *codes_bytes = (size_t)mx_codes_bytes(rows, K, bits);
+    *scales_bytes = (size_t)mx_scales_bytes(rows, K);
+    return FATE_OK;
+}
+
+extern "C" fate_status fate_mx_pack_weight(void* stream, const void* src, int src_type, int rows, int K, int64_t ld_src,
+                                           int bits, void* codes, void* scales) {
+    const fate_status s = check_weight(rows, K, bits);
+    if (s != FATE_OK) return s;
+    if (!plain_type(src_type)) FATE_FAIL(FATE_EINVAL, "src_type = %d (FATE_BF16 or FATE_FP32)", src_type);
+    if (ld_src < K) FATE_FAIL(FATE_ESHAPE, "rows lie at least K = %d elements apart", K);
+    FATE_CHECK_PTR(src);
+    FATE_CHECK_PTR(codes);
+    FATE_CHECK_PTR(scales);
+    const long long n = (long long)mx_row_tiles(rows) * 16 * mx_step_groups(K) * 16;
+    const long long grid = (n + 255) / 256;
+    if (grid > 0x7fffffffLL) FATE_FAIL(FATE_ESHAPE, "matrix too large");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    uint8_t* c = static_cast<uint8_t*>(codes);
+    uint8_t* sc = static_cast<uint8_t*>(scales);
+    if (src_type == FATE_FP32)
+        mx_pack_weight_kernel<float><<<(unsigned)grid, 256, 0, st>>>(static_cast<const float*>(src), ld_src, rows, K, bits, c, sc);
+    else
+        mx_pack_weight_kernel<uint16_t><<<(unsigned)grid, 256, 0, st>>>(static_cast<const uint16_t*>(src), ld_src, rows, K, bits, c, sc);
+    FATE_HIP(hipGetLastError());
+    return FATE_OK;
+}

@@ -1,0 +1,373 @@
+// Products with block-scaled weights for few rows: weights go from memory straight into the matrix instruction's
+// registers, the rows wait in LDS.
+#include "mx_gemm.h"
+
+namespace fate {
+
+constexpr int kStreamWaves = 8;
+constexpr int kStreamRing = 8;          // weight tiles in flight per wave
+
+// The wave's tiles s0 .. s1 - 1 of one tile row, multiplied with the rows in LDS.
+// xl [rows][Kp + 16] codes, sl [rows][Kp / 32] scales; rows behind the last one read row 0 (their sums are not stored).
+template <int BITS, typename Stage>
+__device__ __forceinline__ v4f stream_tiles(const uint8_t* w, const uint8_t* ws, int s0, int s1, int Kp,
+                                            const uint8_t* xl, const uint8_t* sl, int rows, Stage stage) {
+    const int lane = (int)(threadIdx.x & 63), g = lane >> 4;
+    MxWTile<BITS> wt[kStreamRing];
+    uint32_t sc[kStreamRing];
+    const uint32_t* wsd = reinterpret_cast<const uint32_t*>(ws) + lane;
+    const int n = s1 - s0;
+    if (n > 0) {
+#pragma unroll
+        for (int j = 0; j < kStreamRing; ++j) {
+            const int s = s0 + (j < n ? j : n - 1);
+            wt[j].load(w + (long long)s * MxWTile<BITS>::kBytes, lane);
+            sc[j] = wsd[(s >> 2) * 64];
+        }
+    }
+    stage();                             // rows into LDS while the weights travel
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (n > 0) {
+        const int row = (lane & 15) < rows ? lane & 15 : 0;
+        const uint8_t* xr = xl + row * (Kp + 16) + 16 * g;
+        const uint8_t* sr = sl + row * (Kp / 32) + g;
+        for (int base = s0;; base += kStreamRing) {
+            const bool more = base + kStreamRing < s1;
+#pragma unroll
+            for (int j = 0; j < kStreamRing; ++j) {
+                const int s = base + j;
+                if (s < s1) {
+                    const v4i lo = *reinterpret_cast<const v4i*>(xr + s * kMxStep);
+                    const v4i hi = *reinterpret_cast<const v4i*>(xr + s * kMxStep + 64);
+                    const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    acc = wt[j].template mfma<0>(sc[j] >> (8 * (s & 3)), x, sr[s * 4], acc);
+                }
+                if (more) {
+                    const int t = s + kStreamRing < s1 ? s + kStreamRing : s1 - 1;
+                    wt[j].load(w + (long long)t * MxWTile<BITS>::kBytes, lane);
+                    sc[j] = wsd[(t >> 2) * 64];
+                }
+            }
+            if (!more) break;
+        }
+    }
+    return acc;
+}
+
+// A workgroup of eight waves takes 16 rows of a group and 8 / KS tile rows of weights (UP: two of W1 and the same two of
+// W3, KS = 2); KS waves share the reduction of a tile row and their sums meet in LDS.
+template <bool UP, int KS>
+__global__ __launch_bounds__(64 * kStreamWaves, 2) void mx_stream_kernel(MxArgs a, int cb_r, int cb_s, int rows_cap) {
+    constexpr int NT = kStreamWaves / KS;
+    extern __shared__ __align__(16) uint8_t lds[];
+    v4f* red = reinterpret_cast<v4f*>(lds);                       // [8 waves][64 lanes]
+    uint8_t* xl = lds + kStreamWaves * 64 * sizeof(v4f);
+    const MxItem it = mx_find_item<16, false>(a, cb_r, cb_s, (int)blockIdx.x);
+    if (it.group < 0) return;
+    const bool shared = it.group >= a.E;
+    const int Kp = shared ? a.Kp_s : a.Kp_r;
+    uint8_t* sl = xl + rows_cap * (Kp + 16);
+    MxMatrix m;
+    const bool ok = mx_matrix<UP>(a, it.group, &m);
+    const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int tile = wave / KS, ks = wave % KS;
+    const long long out0 = shared ? (long long)(it.group - a.E) * a.N + it.row0 : it.row0;   // first output row
+    if (!ok) {
+        if (!UP && ks == 0 && (lane & 15) < it.rows) {
+            const int r0 = (it.col * NT + tile) * 16 + 4 * g;
+            const int cols = shared ? a.cols_s : a.cols_r;
+            mx_store_y(a, shared ? a.y_s : a.y_r, (out0 + (lane & 15)) * (shared ? a.ld_s : a.ld_r) + r0, cols - r0,
+                       v4f{0.0f, 0.0f, 0.0f, 0.0f});
+        }
+        return;
+    }
+    auto stage = [&]() {
+        const uint8_t* xb = shared ? a.x_s : a.x_r;
+        const uint8_t* xsb = shared ? a.xs_s : a.xs_r;
+        const int per_row = Kp / 16, pieces = it.rows * per_row;
+        for (int q = (int)threadIdx.x; q < pieces; q += 64 * kStreamWaves) {
+            const int r = q / per_row, c = q - r * per_row;
+            const long long src = shared ? (a.gather ? it.row0 + r : out0 + r)
+                                         : (a.gather ? a.perm[it.row0 + r] / a.k : it.row0 + r);
+            *reinterpret_cast<v4i*>(xl + r * (Kp + 16) + 16 * c) = reinterpret_cast<const v4i*>(xb + src * Kp)[c];
+            if ((c & 7) == 0)
+                *reinterpret_cast<uint32_t*>(sl + r * (Kp / 32) + c / 2) =
+                    reinterpret_cast<const uint32_t*>(xsb + src * (Kp / 32))[c / 8];
+        }
+        __syncthreads();
+    };
+    const int last = mx_row_tiles(m.rows) - 1;
+    int rb = UP ? it.col * 2 + (tile & 1) : it.col * NT + tile;
+    rb = rb < last ? rb : last;
+    const bool third = UP && tile >= 2;
+    const uint8_t* w = (third ? m.w3 : m.w) + (long long)rb * m.KT * (m.bits == 4 ? 1024 : 2048);
+    const uint8_t* ws = (third ? m.s3 : m.s) + (long long)rb * m.KG * 256;
+    const int s0 = m.KT * ks / KS, s1 = m.KT * (ks + 1) / KS;
+    v4f acc;
+    if (m.bits == 4) acc = stream_tiles<4>(w, ws, s0, s1, Kp, xl, sl, it.rows, stage);
+    else acc = stream_tiles<8>(w, ws, s0, s1, Kp, xl, sl, it.rows, stage);
+    if constexpr (KS > 1 || UP) {
+        red[wave * 64 + lane] = acc;
+        __syncthreads();
+    }
+    if constexpr (UP) {
+        if (wave != 0) return;
+        v4f v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = red[i * KS * 64 + lane];
+#pragma unroll
+            for (int p = 1; p < KS; ++p) v[i] += red[(i * KS + p) * 64 + lane];
+        }
+        const int n0 = it.col * 32;
+        v4f h0, h1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool zero = n0 >= m.rows;                       // padding columns of h
+            h0[i] = zero ? 0.0f : mx_swiglu(v[0][i], v[2][i]);
+            h1[i] = zero ? 0.0f : mx_swiglu(v[1][i], v[3][i]);
+        }
+        const long long row = out0 + (lane & 15), ld = shared ? a.ld_s : a.ld_r;
+        mx_store_h(h0, h1, (lane & 15) < it.rows, static_cast<uint8_t*>(shared ? a.y_s : a.y_r) + row * ld + n0,
+                   (shared ? a.ys_s : a.ys_r) + row * (ld / 32) + n0 / 32);
+    } else {
+        if (ks != 0) return;
+#pragma unroll
+        for (int p = 1; p < KS; ++p) acc += red[(wave + p) * 64 + lane];
+        const int r0 = (it.col * NT + tile) * 16 + 4 * g;
+        const int cols = shared ? a.cols_s : a.cols_r;
+        if ((lane & 15) < it.rows && r0 < cols) {
+            if (a.bias != nullptr) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] += r0 + i < cols ? a.bias[r0 + i] : 0.0f;
+            }
+            mx_store_y(a, shared ? a.y_s : a.y_r, (out0 + (lane & 15)) * (shared ? a.ld_s : a.ld_r) + r0, cols - r0, acc);
+        }
+    }
+}
+
+// ---- bf16 rows: weights become the bf16 numbers they are ----------------------------------------------------------
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float mx_scale_f32(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
+
+template <int SEL4>
+__device__ __forceinline__ v2bf mx_pair4(uint32_t d, float s) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, s, SEL4); }
+
+// Eight of a lane's 32 weights: columns 8 j .. + 7 of its own order.
+template <int BITS>
+__device__ __forceinline__ v8bf mx_eight(const MxWTile<BITS>& t, int j, float s) {
+    v2bf p[4];
+    if constexpr (BITS == 4) {
+        const uint32_t d = (uint32_t)t.v[j];
+        p[0] = mx_pair4<0>(d, s); p[1] = mx_pair4<1>(d, s); p[2] = mx_pair4<2>(d, s); p[3] = mx_pair4<3>(d, s);
+    } else {
+        const uint32_t a = (uint32_t)t.v[2 * j], b = (uint32_t)t.v[2 * j + 1];
+        p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false);
+        p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true);
+        p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false);
+        p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
+    }
+    v8bf r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = p[i >> 1][i & 1];
+    return r;
+}
+
+struct MxBf16Args {
+    const uint16_t* x; long long ld_x;
+    MxMatrix m;
+    const float* bias;
+    void* y; long long ld_y;
+    int N, K, R, y_fp32, y_vec, x_vec;
+    int rows_cap, passes;               // tokens per pass
+};
+
+template <int BITS, int KS>
+__global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf16Args a) {
+    constexpr int NT = kStreamWaves / KS;
+    extern __shared__ __align__(16) uint8_t lds[];
+    v4f* red = reinterpret_cast<v4f*>(lds);
+    uint16_t* xl = reinterpret_cast<uint16_t*>(lds + kStreamWaves * 64 * sizeof(v4f));
+    const int col = (int)(blockIdx.x / a.passes), pass = (int)(blockIdx.x - (unsigned)col * a.passes);
+    const int t0 = pass * a.rows_cap, rows = a.N - t0 < a.rows_cap ? a.N - t0 : a.rows_cap;
+    const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int tile = wave / KS, ks = wave % KS;
+    const int KT = a.m.KT, ldx = KT * kMxStep + 8;
+    const int last = mx_row_tiles(a.R) - 1;
+    int rb = col * NT + tile;
+    rb = rb < last ? rb : last;
+    const uint8_t* w = a.m.w + (long long)rb * KT * MxWTile<BITS>::kBytes;
+    const uint32_t* wsd = reinterpret_cast<const uint32_t*>(a.m.s + (long long)rb * a.m.KG * 256) + lane;
+    const int s0 = KT * ks / KS, s1 = KT * (ks + 1) / KS, n = s1 - s0;
+    MxWTile<BITS> wt[kStreamRing];
+    uint32_t sc[kStreamRing];
+    if (n > 0) {
+#pragma unroll
+        for (int j = 0; j < kStreamRing; ++j) {
+            const int s = s0 + (j < n ? j : n - 1);
+            wt[j].load(w + (long long)s * MxWTile<BITS>::kBytes, lane);
+            sc[j] = wsd[(s >> 2) * 64];
+        }
+    }
+    const int per_row = KT * 16, pieces = rows * per_row;         // of eight elements
+    for (int q = (int)threadIdx.x; q < pieces; q += 64 * kStreamWaves) {
+        const int r = q / per_row, i = (q - r * per_row) * 8;
+        const uint16_t* src = a.x + (t0 + r) * a.ld_x + i;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (a.x_vec && i + 8 <= a.K) v = *reinterpret_cast<const uint4*>(src);
+        else {
+            uint32_t d[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i + e < a.K) d[e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
+            v = make_uint4(d[0], d[1], d[2], d[3]);
+        }
+        *reinterpret_cast<uint4*>(xl + r * ldx + i) = v;
+    }
+    __syncthreads();
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (n > 0) {
+        const int row = (lane & 15) < rows ? lane & 15 : 0;
+        const uint16_t* xr = xl + row * ldx + (BITS == 4 ? 32 : 16) * g;
+        for (int base = s0;; base += kStreamRing) {
+            const bool more = base + kStreamRing < s1;
+#pragma unroll
+            for (int j = 0; j < kStreamRing; ++j) {
+                const int s = base + j;
+                if (s < s1) {
+                    // the lane's codes all belong to one row; 8-bit ones to two blocks of it
+                    const uint32_t d = sc[j] >> (8 * (s & 3));
+                    float f0, f1;
+                    if constexpr (BITS == 4) f0 = f1 = mx_scale_f32(d & 255u);
+                    else {
+                        // scale of lane l is that of block l / 16; pieces 16 g and 64 + 16 g lie in blocks g / 2 and 2 + g / 2
+                        f0 = mx_scale_f32((uint32_t)__shfl((int)d, (lane & 15) + 16 * (g >> 1)) & 255u);
+                        f1 = mx_scale_f32((uint32_t)__shfl((int)d, (lane & 15) + 16 * (2 + (g >> 1))) & 255u);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int off = BITS == 4 ? 8 * i : 64 * (i >> 1) + 8 * (i & 1);
+                        const v8bf x = *reinterpret_cast<const v8bf*>(xr + s * kMxStep + off);
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_eight<BITS>(wt[j], i, i < 2 ? f0 : f1), x, acc, 0, 0, 0);
+                    }
+                }
+                if (more) {
+                    const int t = s + kStreamRing < s1 ? s + kStreamRing : s1 - 1;
+                    wt[j].load(w + (long long)t * MxWTile<BITS>::kBytes, lane);
+                    sc[j] = wsd[(t >> 2) * 64];
+                }
+            }
+            if (!more) break;
+        }
+    }
+    if constexpr (KS > 1) {
+        red[wave * 64 + lane] = acc;
+        __syncthreads();
+        if (ks != 0) return;
+#pragma unroll
+        for (int p = 1; p < KS; ++p) acc += red[(wave + p) * 64 + lane];
+    }
+    const int r0 = (col * NT + tile) * 16 + 4 * g;
+    if ((lane & 15) < rows && r0 < a.R) {
+        if (a.bias != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += r0 + i < a.R ? a.bias[r0 + i] : 0.0f;
+        }
+        MxArgs o{};
+        o.y_fp32 = a.y_fp32;
+        o.y_vec = a.y_vec;
+        mx_store_y(o, a.y, (t0 + (lane & 15)) * a.ld_y + r0, a.R - r0, acc);
+    }
+}
+
+constexpr int kRedBytes = kStreamWaves * 64 * 16;
+constexpr int kMaxLds = 144 * 1024;
+
+template <typename F>
+static fate_status allow_lds(F kernel, size_t bytes) {
+    if (bytes > 64 * 1024)
+        FATE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    return FATE_OK;
+}
+
+// How many waves share a reduction: as few as leave about two workgroups per compute unit, each with two steps or more.
+int mx_k_split(long long tiles, int KT) {
+    int ks = 1;
+    while (ks < 8 && tiles * ks / 8 < 512 && KT >= 4 * ks) ks *= 2;
+    return ks;
+}
+
+// Rows of a group that the workgroups keep in LDS; 0: they do not fit.
+int mx_stream_rows(long long rows, int Kp) {
+    const int cap = rows < 16 ? (int)rows : 16;
+    return (long long)cap * (Kp + 16 + Kp / 32) + kRedBytes <= 80 * 1024 ? cap : 0;
+}
+
+long long mx_max_tiles(const MxArgs& a, int RT) {
+    const long long P = (long long)a.N * a.k;
+    return a.E ? P / RT + (P < a.E ? P : a.E) : 0;
+}
+
+fate_status launch_mx_stream(hipStream_t st, const MxArgs& a, bool up, int rows_cap) {
+    const int Kp = a.Kp_r > a.Kp_s ? a.Kp_r : a.Kp_s;
+    const size_t lds = kRedBytes + (size_t)rows_cap * (Kp + 16 + Kp / 32);
+    const long long tr = mx_max_tiles(a, 16), ts = (long long)a.n_shared * ((a.N + 15) / 16);
+    auto go = [&](auto kernel, int width) -> fate_status {
+        const int cb_r = (a.cols_r + width - 1) / width, cb_s = (a.cols_s + width - 1) / width;
+        const long long grid = tr * cb_r + ts * cb_s;
+        if (grid > 0x7fffffffLL) FATE_FAIL(FATE_ESHAPE, "too many workgroups (%lld)", grid);
+        const fate_status s = allow_lds(kernel, lds);
+        if (s != FATE_OK) return s;
+        kernel<<<(unsigned)grid, 64 * kStreamWaves, lds, st>>>(a, cb_r, cb_s, rows_cap);
+        FATE_HIP(hipGetLastError());
+        return FATE_OK;
+    };
+    if (up) return go(mx_stream_kernel<true, 2>, 32);
+    const int KT = Kp / kMxStep;
+    const int ks = mx_k_split(tr * ((a.cols_r + 15) / 16) + ts * ((a.cols_s + 15) / 16), KT);
+    switch (ks) {
+        case 1: return go(mx_stream_kernel<false, 1>, 128);
+        case 2: return go(mx_stream_kernel<false, 2>, 64);
+        case 4: return go(mx_stream_kernel<false, 4>, 32);
+        default: return go(mx_stream_kernel<false, 8>, 16);
+    }
+}
+
+fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x, const MxMatrix& m, const float* bias,
+                                  void* y, long long ld_y, int N, int K, int R, int y_fp32, int y_vec) {
+    MxBf16Args a{};
+    a.x = static_cast<const uint16_t*>(x); a.ld_x = ld_x; a.m = m; a.bias = bias; a.y = y; a.ld_y = ld_y;
+    a.N = N; a.K = K; a.R = R; a.y_fp32 = y_fp32; a.y_vec = y_vec;
+    a.x_vec = ld_x % 8 == 0;
+    const int row_bytes = (m.KT * kMxStep + 8) * 2;
+    a.rows_cap = (kMaxLds - kRedBytes) / row_bytes;
+    if (a.rows_cap > 16) a.rows_cap = 16;
+    if (a.rows_cap > N) a.rows_cap = N;
+    if (a.rows_cap < 1) FATE_FAIL(FATE_ESHAPE, "K = %d: a bf16 row does not fit into LDS (K <= 65536)", K);
+    a.passes = (N + a.rows_cap - 1) / a.rows_cap;
+    const size_t lds = kRedBytes + (size_t)a.rows_cap * row_bytes;
+    const int ks = mx_k_split((long long)a.passes * ((R + 15) / 16), m.KT);
+    auto go = [&](auto kernel, int width) -> fate_status {
+        const long long grid = (long long)((R + width - 1) / width) * a.passes;
+        if (grid > 0x7fffffffLL) FATE_FAIL(FATE_ESHAPE, "too many workgroups (%lld)", grid);
+        const fate_status s = allow_lds(kernel, lds);
+        if (s != FATE_OK) return s;
+        kernel<<<(unsigned)grid, 64 * kStreamWaves, lds, st>>>(a);
+        FATE_HIP(hipGetLastError());
+        return FATE_OK;
+    };
+#define FATE_BY_SPLIT(B)                                             \
+    switch (ks) {                                                    \
+        case 1: return go(mx_linear_bf16_kernel<B, 1>, 128);         \
+        case 2: return go(mx_linear_bf16_kernel<B, 2>, 64);          \
+        case 4: return go(mx_linear_bf16_kernel<B, 4>, 32);          \
+        default: return go(mx_linear_bf16_kernel<B, 8>, 16);         \
+    }
+    if (m.bits == 4) FATE_BY_SPLIT(4) else FATE_BY_SPLIT(8)
+#undef FATE_BY_SPLIT
+}
+
+}  // namespace fate

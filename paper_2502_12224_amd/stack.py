@@ -8,8 +8,8 @@ import ctypes as C
 import torch
 
 from . import binding as B
-from workloads import (MoEShape, chain_next_hidden, gen_expert, gen_gate, gen_hidden, gen_shared_gate,
-                       unit_rmsnorm_bf16)
+from workloads import (MoEShape, chain_next_hidden, gen_expert, gen_expert_unquantized, gen_gate, gen_hidden,
+                       gen_shared_gate, unit_rmsnorm_bf16)
 
 
 class LayerWeights:
@@ -81,7 +81,14 @@ def layer_forward(cfg: MoEShape, lw: LayerWeights, lw_next, x, buf: LayerBuffers
                                 buf.inv_perm, buf.order, lw.table, lw.shared_table, lw.shared_gate, buf.y,
                                 buf.layer_ws, hint_ids=hint_ids)
         return buf.y
-    fused = buf.fused_ok if fused is None else fused
+    _route(cfg, lw, lw_next, x, buf, buf.fused_ok if fused is None else fused)
+    B.fate_moe_ffn_q(buf.desc, x, lw.table, buf.counts, buf.offsets, buf.perm, buf.inv_perm, buf.order, buf.w,
+                     lw.shared_table, lw.shared_gate, buf.y, buf.ffn_ws)
+    return buf.y
+
+
+def _route(cfg, lw, lw_next, x, buf, fused):
+    """Routing, prediction and permutation of one layer into buf's outputs."""
     if fused:
         B.fate_route_fused(x, lw.Wg, lw.bias, None if lw_next is None else lw_next.Wg,
                            None if lw_next is None else lw_next.bias, cfg.k, cfg.m, cfg.renorm, buf.ids, buf.w,
@@ -93,9 +100,88 @@ def layer_forward(cfg: MoEShape, lw: LayerWeights, lw_next, x, buf: LayerBuffers
             B.fate_cross_layer_predict(x, lw_next.Wg, lw_next.bias, cfg.k, cfg.m, buf.pred_ids, buf.pred_w,
                                        buf.pred_pop)
         B.fate_permute(buf.ids, cfg.E, buf.counts, buf.offsets, buf.perm, buf.inv_perm, buf.order)
-    B.fate_moe_ffn_q(buf.desc, x, lw.table, buf.counts, buf.offsets, buf.perm, buf.inv_perm, buf.order, buf.w,
-                     lw.shared_table, lw.shared_gate, buf.y, buf.ffn_ws)
+
+
+class MxLayerWeights:
+    """One layer whose experts are stored as block-scaled 4- or 8-bit values."""
+
+    def __init__(self, cfg: MoEShape, layer: int, device):
+        self.Wg, self.bias = gen_gate(cfg, layer, device)
+        self.shared_gate = gen_shared_gate(cfg, layer, device)
+        self.norm = torch.ones(cfg.H, dtype=torch.bfloat16, device=device)
+
+        def pack(e, shared, bits):
+            return B.MxExpert(*(B.MxWeight(w, bits) for w in gen_expert_unquantized(cfg, layer, e, shared, device)))
+        self.experts = [pack(e, False, cfg.bits) for e in range(cfg.E)]
+        self.shared = [pack(v, True, cfg.shared_bits) for v in range(cfg.n_shared)]
+        self.table = B.expert_table([e.struct() for e in self.experts], device)
+        self.shared_table = B.expert_table([e.struct() for e in self.shared], device) if cfg.n_shared else None
+
+    def nbytes(self):
+        return sum(e.nbytes() for e in self.experts + self.shared)
+
+
+class MxBuffers:
+    """Rows, routing outputs and FFN output of one layer on block-scaled experts, for N tokens."""
+
+    def __init__(self, cfg: MoEShape, N: int, device, y_is_fp32=True):
+        E, k, m, H = cfg.E, cfg.k, cfg.m, cfg.H
+        i32 = dict(dtype=torch.int32, device=device)
+        f32 = dict(dtype=torch.float32, device=device)
+        self.x = torch.zeros(N, H, dtype=torch.bfloat16, device=device)
+        self.mx = B.mx_empty(N, H, device)
+        self.ids, self.w = torch.zeros(N, k, **i32), torch.zeros(N, k, **f32)
+        self.pred_ids, self.pred_w = torch.zeros(N, m, **i32), torch.zeros(N, m, **f32)
+        self.pred_pop, self.counts, self.order = (torch.zeros(E, **i32) for _ in range(3))
+        self.offsets = torch.zeros(E + 1, **i32)
+        self.perm, self.inv_perm = (torch.zeros(max(N * k, 1), **i32) for _ in range(2))
+        self.y = torch.zeros(N, H, dtype=torch.float32 if y_is_fp32 else torch.bfloat16, device=device)
+        self.desc = B.make_ffn_desc(N, H, E, k, cfg.I, cfg.bits, B.MX_GROUP, cfg.n_shared, cfg.I_shared or 0,
+                                    cfg.shared_bits, B.MX_GROUP, y_is_fp32)
+        self.ffn_ws = torch.zeros(B.fate_moe_ffn_mx_workspace(self.desc), dtype=torch.uint8, device=device)
+        self.fused_ok = 1 <= N <= 16 or (N >= 64 and H % 1024 == 0)
+        self.route_ws = torch.zeros(B.fate_route_fused_workspace(max(N, 1), E), dtype=torch.uint8, device=device)
+
+    def status(self):
+        """Status word of the FFN calls so far (0 = fine)."""
+        return int(self.ffn_ws[:4].view(torch.int32)[0])
+
+
+def mx_layer_forward(cfg: MoEShape, lw: MxLayerWeights, lw_next, h, y, buf: MxBuffers, eps=1e-6):
+    """One MoE layer on block-scaled values: the residual stream takes the previous layer's output y (None: nothing) and
+    is normalised into bf16 rows for the gates and 8-bit rows for the experts, in one pass; then routing and FFN."""
+    B.fate_add_rmsnorm(h, y, lw.norm, eps, h_out=None if y is None else h, x=buf.x, mx=buf.mx)
+    _route(cfg, lw, lw_next, buf.x, buf, buf.fused_ok)
+    B.fate_moe_ffn_mx(buf.desc, *buf.mx, lw.table, buf.counts, buf.offsets, buf.perm, buf.inv_perm, buf.order, buf.w,
+                      lw.shared_table, lw.shared_gate, buf.y, buf.ffn_ws)
     return buf.y
+
+
+class MxStack:
+    """Layers of block-scaled experts on the device, and a vocabulary head."""
+
+    def __init__(self, cfg: MoEShape, device="cuda", layers=None, vocabulary=0):
+        self.cfg, self.device = cfg, device
+        self.layers = [MxLayerWeights(cfg, l, device) for l in range(cfg.layers if layers is None else layers)]
+        self.norm = torch.ones(cfg.H, dtype=torch.bfloat16, device=device)
+        self.head = None
+        if vocabulary:
+            g = torch.Generator(device=device)
+            g.manual_seed(cfg.seed * 7919 + 11)
+            w = torch.randn(vocabulary, cfg.H, generator=g, device=device) / cfg.H ** 0.5
+            self.head = B.MxWeight(w, cfg.bits)
+
+    def forward(self, h, buf: MxBuffers, logits=None):
+        """h [N, H] (the residual stream, updated in place) through all layers; the logits [N, vocabulary] of the head."""
+        y = None
+        for l, lw in enumerate(self.layers):
+            y = mx_layer_forward(self.cfg, lw, self.layers[l + 1] if l + 1 < len(self.layers) else None, h, y, buf)
+        B.fate_add_rmsnorm(h, y, self.norm, h_out=h, x=buf.x)
+        if self.head is not None:
+            if logits is None:
+                logits = torch.empty(h.shape[0], self.head.R, dtype=torch.float32, device=h.device)
+            B.fate_mx_linear(buf.x, self.head, logits)
+        return logits
 
 
 class MoEStack:
