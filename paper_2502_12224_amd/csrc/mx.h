@@ -32,6 +32,13 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
+// A load from memory through a pointer that the compiler cannot trace to a kernel argument (expert tables hold them): as a
+// flat load it would count as an LDS access too, and every wait for it would be a wait for everything.
+template <typename T>
+__device__ __forceinline__ T ld_global(const void* p, long long i = 0) {
+    return reinterpret_cast<const __attribute__((address_space(1))) T*>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
 // Bits of |v|: they order like the values, and NaN and infinity come out on top.
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 

@@ -27,41 +27,57 @@ __device__ __forceinline__ v4f row4(const void* rows, long long at) {
 }
 
 // y[t] = sum_j w[t,j] row[inv_perm[t,j]] + g(t) sum_v shared row: one workgroup per token, terms in the order of j, then v.
+// The rows are requested before the gate is known; what is left is two round trips and the launch.
 template <typename T>
-__global__ __launch_bounds__(256) void mx_combine_kernel(MxCombineArgs a) {
-    __shared__ float part[4];
+__global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
+    __shared__ float part[16];
     const long long t = blockIdx.x;
-    float gate = 1.0f;
+    const int P = a.N * a.k, threads = (int)blockDim.x;
+    float dot = 0.0f;
     if (a.gate != nullptr) {
-        float s = 0.0f;
-        for (int i = (int)threadIdx.x * 4; i < a.H; i += 1024) {
+        for (int i = (int)threadIdx.x * 4; i < a.H; i += threads * 4) {
             const int c = *reinterpret_cast<const int*>(a.x + t * a.Kp + i);
             const uint32_t b = a.xs[(t * a.Kp + i) / kMxBlock];
             const float f = b == 255u ? __builtin_nanf("") : __uint_as_float(b ? b << 23 : 0x400000u);
             const uint2 w = *reinterpret_cast<const uint2*>(a.gate + i);
-            s += f * (__builtin_amdgcn_cvt_f32_fp8(c, 0) * bf16_lo(w.x) + __builtin_amdgcn_cvt_f32_fp8(c, 1) * bf16_hi(w.x) +
-                      __builtin_amdgcn_cvt_f32_fp8(c, 2) * bf16_lo(w.y) + __builtin_amdgcn_cvt_f32_fp8(c, 3) * bf16_hi(w.y));
+            dot += f * (__builtin_amdgcn_cvt_f32_fp8(c, 0) * bf16_lo(w.x) + __builtin_amdgcn_cvt_f32_fp8(c, 1) * bf16_hi(w.x) +
+                        __builtin_amdgcn_cvt_f32_fp8(c, 2) * bf16_lo(w.y) + __builtin_amdgcn_cvt_f32_fp8(c, 3) * bf16_hi(w.y));
         }
-        s = wave_sum(s);
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
-        __syncthreads();
-        gate = 1.0f / (1.0f + __expf(-((part[0] + part[1]) + (part[2] + part[3]))));
     }
-    const int P = a.N * a.k;
-    for (int i = (int)threadIdx.x * 4; i < a.H; i += 1024) {
-        v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (int j = 0; j < a.k; ++j) {
-            const int s = a.inv_perm[t * a.k + j];
-            const float w = a.topk_w[t * a.k + j];
-            if ((unsigned)s < (unsigned)P) y += w * row4<T>(a.rows_r, (long long)s * a.H + i);
+    float gate = 1.0f;
+    for (int i0 = 0; i0 < a.H; i0 += threads * 4) {
+        const int i = i0 + (int)threadIdx.x * 4;
+        v4f y = {0.0f, 0.0f, 0.0f, 0.0f}, z = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (i < a.H) {
+            for (int j0 = 0; j0 < a.k; j0 += 8) {
+                int s[8];
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int at = j0 + j < a.k ? j0 + j : a.k - 1;
+                    s[j] = a.inv_perm[t * a.k + at];
+                    w[j] = a.topk_w[t * a.k + at];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j0 + j < a.k && (unsigned)s[j] < (unsigned)P) y += w[j] * row4<T>(a.rows_r, (long long)s[j] * a.H + i);
+            }
+            for (int v = 0; v < a.n_shared; ++v) z += row4<T>(a.rows_s, ((long long)v * a.N + t) * a.H + i);
         }
-        v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int v = 0; v < a.n_shared; ++v) z += row4<T>(a.rows_s, ((long long)v * a.N + t) * a.H + i);
+        if (a.gate != nullptr && i0 == 0) {
+            dot = wave_sum(dot);
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = dot;
+            __syncthreads();
+            dot = 0.0f;
+            for (int p = 0; p < threads / 64; ++p) dot += part[p];
+            gate = 1.0f / (1.0f + __expf(-dot));
+        }
         y += gate * z;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f*>(static_cast<float*>(a.y) + t * a.H + i) = y;
-        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.H + i) =
-                 make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+        if (i < a.H) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f*>(static_cast<float*>(a.y) + t * a.H + i) = y;
+            else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.H + i) =
+                     make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+        }
     }
 }
 
@@ -218,8 +234,9 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     MxCombineArgs c{base + w.rows_r, base + w.rows_s, inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
                     static_cast<const uint8_t*>(x_scales), d->n_shared ? static_cast<const uint16_t*>(shared_gate_bf16) : nullptr,
                     y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H)};
-    if (d->y_is_fp32) mx_combine_kernel<float><<<d->N, 256, 0, st>>>(c);
-    else mx_combine_kernel<uint16_t><<<d->N, 256, 0, st>>>(c);
+    const int threads = d->H >= 4096 ? 1024 : (d->H + 255) / 256 * 64;
+    if (d->y_is_fp32) mx_combine_kernel<float><<<d->N, threads, 0, st>>>(c);
+    else mx_combine_kernel<uint16_t><<<d->N, threads, 0, st>>>(c);
     FATE_HIP(hipGetLastError());
     return FATE_OK;
 }

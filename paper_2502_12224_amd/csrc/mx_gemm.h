@@ -36,6 +36,32 @@ struct MxArgs {
 
 
 #ifdef __HIPCC__
+// Values that all lanes agree on, as the compiler is told: in scalar registers, branches on them scalar too.
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ long long uni(long long v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((unsigned long long)v >> 32));
+    return (long long)(((unsigned long long)hi << 32) | lo);
+}
+template <typename T>
+__device__ __forceinline__ T* uni(T* p) { return reinterpret_cast<T*>((uintptr_t)uni((long long)reinterpret_cast<uintptr_t>(p))); }
+// By value: a choice between two members would be a choice between their addresses, and the arguments went to memory.
+template <typename T>
+__device__ __forceinline__ T pick(bool c, T a, T b) { return c ? a : b; }
+
+// What a group of rows reads and writes.
+struct MxSide {
+    const uint8_t* x; const uint8_t* xs;
+    void* y; uint8_t* ys;
+    long long ld;
+    int Kp, cols;
+};
+__device__ __forceinline__ MxSide mx_side(const MxArgs& a, bool shared) {
+    return MxSide{pick(shared, a.x_s, a.x_r), pick(shared, a.xs_s, a.xs_r), pick(shared, a.y_s, a.y_r),
+                  pick(shared, a.ys_s, a.ys_r), pick(shared, a.ld_s, a.ld_r), pick(shared, a.Kp_s, a.Kp_r),
+                  pick(shared, a.cols_s, a.cols_r)};
+}
+
 // The piece of work number `item`: shared groups first (their reductions are the long ones), then the experts; within
 // a group the row tiles of one column block follow each other.
 struct MxItem {
@@ -56,7 +82,7 @@ __device__ __forceinline__ int wave_scan_inclusive(int v) {
 // Every wave of a workgroup works this out for itself (no barrier); E <= 256: four experts per lane.
 // xcd: spread over eight contiguous ranges, one per die, so that the row tiles of a column block share an L2.
 template <int RT, bool XCD>
-__device__ __forceinline__ MxItem mx_find_item(const MxArgs& a, int cb_r, int cb_s, int bid) {
+__device__ __forceinline__ MxItem mx_locate(const MxArgs& a, int cb_r, int cb_s, int bid) {
     const int lane = (int)(threadIdx.x & 63);
     const int tiles_s = (a.N + RT - 1) / RT;
     const int n_s = a.n_shared * tiles_s * cb_s;
@@ -64,7 +90,7 @@ __device__ __forceinline__ MxItem mx_find_item(const MxArgs& a, int cb_r, int cb
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
         const int e = lane * 4 + i;
-        o[i] = a.E > 0 ? a.offsets[e < a.E ? e : a.E] : 0;
+        o[i] = a.E > 0 ? ld_global<int>(a.offsets, e < a.E ? e : a.E) : 0;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -114,7 +140,13 @@ __device__ __forceinline__ MxItem mx_find_item(const MxArgs& a, int cb_r, int cb
     return r;
 }
 
-// The matrix of an item; false (and a status bit) if the entry cannot be used.
+template <int RT, bool XCD>
+__device__ __forceinline__ MxItem mx_find_item(const MxArgs& a, int cb_r, int cb_s, int bid) {
+    const MxItem r = mx_locate<RT, XCD>(a, cb_r, cb_s, bid);
+    return MxItem{uni(r.group), uni(r.col), uni(r.row0), uni(r.rows)};
+}
+
+// The matrix of an item; false (and a status bit) if the entry cannot be used.  An entry is read in one piece.
 template <bool UP>
 __device__ __forceinline__ bool mx_matrix(const MxArgs& a, int group, MxMatrix* m) {
     if (a.direct.w != nullptr) {
@@ -122,25 +154,33 @@ __device__ __forceinline__ bool mx_matrix(const MxArgs& a, int group, MxMatrix* 
         return true;
     }
     const bool shared = group >= a.E;
-    const fate_qexpert& e = shared ? a.shared[group - a.E] : a.experts[group];
-    const int I_max = a.down ? (shared ? a.K_s : a.K_r) : (shared ? a.cols_s : a.cols_r);
+    const fate_qexpert* p = pick(shared, a.shared + (group - a.E), a.experts + group);
+    // w1 w3 | w2 s1 | s3 s2 | bits group I . | z1 ..
+    const v4i q0 = ld_global<v4i>(p, 0), q1 = ld_global<v4i>(p, 1), q2 = ld_global<v4i>(p, 2), q3 = ld_global<v4i>(p, 3),
+              q4 = ld_global<v4i>(p, 4);
+    auto pointer = [](int lo, int hi) {
+        return reinterpret_cast<const uint8_t*>(((unsigned long long)(uint32_t)uni(hi) << 32) | (uint32_t)uni(lo));
+    };
+    const uint8_t* w1 = pointer(q0[0], q0[1]);
+    const int bits = uni(q3[0]), group_size = uni(q3[1]), I = uni(q3[2]);
+    const int I_max = pick(a.down != 0, pick(shared, a.K_s, a.K_r), pick(shared, a.cols_s, a.cols_r));
     int bit = 0;
-    if (e.w1 == nullptr) bit = 1;
-    else if ((e.bits != 4 && e.bits != 8) || e.group != kMxBlock || e.I < kMxBlock || e.I % kMxBlock || e.I > I_max ||
-             e.z1 != nullptr) bit = 4;
+    if (w1 == nullptr) bit = 1;
+    else if ((bits != 4 && bits != 8) || group_size != kMxBlock || I < kMxBlock || I % kMxBlock || I > I_max ||
+             pointer(q4[0], q4[1]) != nullptr) bit = 4;
     if (bit) {
         if (threadIdx.x == 0) atomicOr(a.status, bit);
         return false;
     }
-    const int K = a.down ? e.I : (shared ? a.K_s : a.K_r);
-    m->w = static_cast<const uint8_t*>(a.down ? e.w2 : e.w1);
-    m->s = static_cast<const uint8_t*>(a.down ? e.s2 : e.s1);
-    m->w3 = static_cast<const uint8_t*>(e.w3);
-    m->s3 = static_cast<const uint8_t*>(e.s3);
-    m->bits = e.bits;
+    const int K = pick(a.down != 0, I, pick(shared, a.K_s, a.K_r));
+    m->w = UP ? w1 : pointer(q1[0], q1[1]);
+    m->s = UP ? pointer(q1[2], q1[3]) : pointer(q2[2], q2[3]);
+    m->w3 = pointer(q0[2], q0[3]);
+    m->s3 = pointer(q2[0], q2[1]);
+    m->bits = bits;
     m->KT = mx_steps(K);
     m->KG = mx_step_groups(K);
-    m->rows = a.down ? (shared ? a.cols_s : a.cols_r) : e.I;
+    m->rows = UP ? I : pick(shared, a.cols_s, a.cols_r);
     return true;
 }
 
@@ -158,7 +198,7 @@ __device__ __forceinline__ v4f mx_mfma8(v8i w, uint32_t ws, v8i x, uint32_t xs, 
 template <int BITS> struct MxWTile;                     // a lane's part of a weight tile
 template <> struct MxWTile<4> {
     v4i v;
-    __device__ __forceinline__ void load(const uint8_t* p, int lane) { v = reinterpret_cast<const v4i*>(p)[lane]; }
+    __device__ __forceinline__ void load(const uint8_t* p, int lane) { v = ld_global<v4i>(p, lane); }
     template <int SEL> __device__ __forceinline__ v4f mfma(uint32_t ws, v8i x, uint32_t xs, v4f acc) const {
         return mx_mfma4<SEL>(v, ws, x, xs, acc);
     }
@@ -167,7 +207,7 @@ template <> struct MxWTile<4> {
 template <> struct MxWTile<8> {
     v8i v;
     __device__ __forceinline__ void load(const uint8_t* p, int lane) {
-        const v4i a = reinterpret_cast<const v4i*>(p)[lane], b = reinterpret_cast<const v4i*>(p)[64 + lane];
+        const v4i a = ld_global<v4i>(p, lane), b = ld_global<v4i>(p, 64 + lane);
         v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     template <int SEL> __device__ __forceinline__ v4f mfma(uint32_t ws, v8i x, uint32_t xs, v4f acc) const {
@@ -202,16 +242,16 @@ __device__ __forceinline__ void mx_store_h(const v4f& h0, const v4f& h1, bool li
 }
 
 // Four consecutive outputs of one row.
-__device__ __forceinline__ void mx_store_y(const MxArgs& a, void* y, long long at, int left, v4f v) {
-    if (a.y_fp32) {
+__device__ __forceinline__ void mx_store_y(bool y_fp32, bool y_vec, void* y, long long at, int left, v4f v) {
+    if (y_fp32) {
         float* p = static_cast<float*>(y) + at;
-        if (a.y_vec && left >= 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        if (y_vec && left >= 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
         else
             for (int i = 0; i < 4; ++i)
                 if (i < left) p[i] = v[i];
     } else {
         uint16_t* p = static_cast<uint16_t*>(y) + at;
-        if (a.y_vec && left >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        if (y_vec && left >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
         else
             for (int i = 0; i < 4; ++i)
                 if (i < left) p[i] = (uint16_t)f32_to_bf16_bits(v[i]);

@@ -1,125 +1,167 @@
 // Products with block-scaled weights for few rows: weights go from memory straight into the matrix instruction's
 // registers, the rows wait in LDS.
+#include "async_lds.h"
 #include "mx_gemm.h"
 
 namespace fate {
 
-constexpr int kStreamWaves = 8;
-constexpr int kStreamRing = 8;          // weight tiles in flight per wave
+constexpr int kStreamWaves = 8, kStreamThreads = 64 * kStreamWaves;
+// Weight tiles in flight per wave: 8 KiB in either width.
+template <int BITS> constexpr int kStreamRing = BITS == 4 ? 8 : 4;
+constexpr int kStagePieces = 4;         // pieces of 16 bytes of the rows that a thread requests before any weights
 
-// The wave's tiles s0 .. s1 - 1 of one tile row, multiplied with the rows in LDS.
-// xl [rows][Kp + 16] codes, sl [rows][Kp / 32] scales; rows behind the last one read row 0 (their sums are not stored).
-template <int BITS, typename Stage>
-__device__ __forceinline__ v4f stream_tiles(const uint8_t* w, const uint8_t* ws, int s0, int s1, int Kp,
-                                            const uint8_t* xl, const uint8_t* sl, int rows, Stage stage) {
-    const int lane = (int)(threadIdx.x & 63), g = lane >> 4;
-    MxWTile<BITS> wt[kStreamRing];
-    uint32_t sc[kStreamRing];
-    const uint32_t* wsd = reinterpret_cast<const uint32_t*>(ws) + lane;
-    const int n = s1 - s0;
-    if (n > 0) {
+// The rows of a workgroup on their way into LDS: [rows][Kp + 16] codes (16 bytes more per row: the 16 lanes that read one
+// piece of 16 rows at a time find them on different banks) and [rows][Kp / 32] scales.  Loads return in order, so the
+// rows are requested first, and put into LDS while the weights travel.
+struct MxRowStage {
+    const uint8_t* x; const uint8_t* xs;
+    const int32_t* perm;                // NULL: row r is source row `first` + r
+    long long first;
+    int k, rows, Kp, per_row, pieces;
+    v4i v[kStagePieces];
+    uint32_t sc[kStagePieces];
+
+    __device__ __forceinline__ long long source(int r) const { return perm != nullptr ? ld_global<int>(perm, first + r) / k : first + r; }
+    __device__ __forceinline__ void request(int i, int q) {
+        const int r = q / per_row, c = q - r * per_row;
+        const long long src = source(r);
+        v[i] = ld_global<v4i>(x + src * Kp, c);
+        sc[i] = ld_global<uint32_t>(xs + src * (Kp / 32), c >> 3);
+    }
+    __device__ __forceinline__ void put(int i, int q, uint8_t* xl, uint8_t* sl) const {
+        const int r = q / per_row, c = q - r * per_row;
+        *reinterpret_cast<v4i*>(xl + r * (Kp + 16) + 16 * c) = v[i];
+        if ((c & 7) == 0) *reinterpret_cast<uint32_t*>(sl + r * (Kp / 32) + c / 2) = sc[i];
+    }
+    __device__ __forceinline__ void begin() {
 #pragma unroll
-        for (int j = 0; j < kStreamRing; ++j) {
-            const int s = s0 + (j < n ? j : n - 1);
-            wt[j].load(w + (long long)s * MxWTile<BITS>::kBytes, lane);
-            sc[j] = wsd[(s >> 2) * 64];
+        for (int i = 0; i < kStagePieces; ++i) {
+            const int q = (int)threadIdx.x + i * kStreamThreads;
+            if (i * kStreamThreads < pieces) request(i, q < pieces ? q : pieces - 1);
         }
     }
-    stage();                             // rows into LDS while the weights travel
-    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (n > 0) {
-        const int row = (lane & 15) < rows ? lane & 15 : 0;
-        const uint8_t* xr = xl + row * (Kp + 16) + 16 * g;
-        const uint8_t* sr = sl + row * (Kp / 32) + g;
-        for (int base = s0;; base += kStreamRing) {
-            const bool more = base + kStreamRing < s1;
+    __device__ __forceinline__ void finish(uint8_t* xl, uint8_t* sl) {
 #pragma unroll
-            for (int j = 0; j < kStreamRing; ++j) {
-                const int s = base + j;
-                if (s < s1) {
-                    const v4i lo = *reinterpret_cast<const v4i*>(xr + s * kMxStep);
-                    const v4i hi = *reinterpret_cast<const v4i*>(xr + s * kMxStep + 64);
-                    const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    acc = wt[j].template mfma<0>(sc[j] >> (8 * (s & 3)), x, sr[s * 4], acc);
-                }
-                if (more) {
-                    const int t = s + kStreamRing < s1 ? s + kStreamRing : s1 - 1;
-                    wt[j].load(w + (long long)t * MxWTile<BITS>::kBytes, lane);
-                    sc[j] = wsd[(t >> 2) * 64];
-                }
+        for (int i = 0; i < kStagePieces; ++i) {
+            const int q = (int)threadIdx.x + i * kStreamThreads;
+            if (q < pieces) put(i, q, xl, sl);
+        }
+        for (int q = (int)threadIdx.x + kStagePieces * kStreamThreads; q < pieces; q += kStreamThreads) {
+            request(0, q);
+            put(0, q, xl, sl);
+        }
+        lds_only_barrier();
+    }
+};
+
+// The wave's tiles s0 .. s1 - 1 of one tile row, multiplied with the rows in LDS; rows behind the last one read row 0
+// (their sums are not stored).
+template <int BITS>
+__device__ __forceinline__ v4f stream_tiles(const uint8_t* w, const uint8_t* ws, int s0, int s1, MxRowStage& rows,
+                                            uint8_t* xl, uint8_t* sl) {
+    constexpr int R = kStreamRing<BITS>;
+    const int lane = (int)(threadIdx.x & 63), g = lane >> 4;
+    MxWTile<BITS> wt[R];
+    uint32_t sc[R];
+    const uint32_t* wsd = reinterpret_cast<const uint32_t*>(ws) + lane;
+    const int end = s1 > s0 ? s1 - 1 : s0;          // a wave without tiles reads the first one
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int s = s0 + j < end ? s0 + j : end;
+        wt[j].load(w + (long long)s * MxWTile<BITS>::kBytes, lane);
+        sc[j] = ld_global<uint32_t>(wsd, (s >> 2) * 64);
+    }
+    rows.finish(xl, sl);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int row = (lane & 15) < rows.rows ? lane & 15 : 0;
+    const uint8_t* xr = xl + row * (rows.Kp + 16) + 16 * g;
+    const uint8_t* sr = sl + row * (rows.Kp / 32) + g;
+    for (int base = s0; base < s1; base += R) {
+        const bool more = base + R < s1;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int s = base + j;
+            if (s < s1) {
+                const v4i lo = *reinterpret_cast<const v4i*>(xr + s * kMxStep);
+                const v4i hi = *reinterpret_cast<const v4i*>(xr + s * kMxStep + 64);
+                const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                acc = wt[j].template mfma<0>(sc[j] >> (8 * (s & 3)), x, sr[s * 4], acc);
             }
-            if (!more) break;
+            if (more) {
+                const int t = s + R < end ? s + R : end;
+                wt[j].load(w + (long long)t * MxWTile<BITS>::kBytes, lane);
+                sc[j] = ld_global<uint32_t>(wsd, (t >> 2) * 64);
+            }
         }
     }
     return acc;
 }
 
-// A workgroup of eight waves takes 16 rows of a group and 8 / KS tile rows of weights (UP: two of W1 and the same two of
-// W3, KS = 2); KS waves share the reduction of a tile row and their sums meet in LDS.
+// A workgroup of eight waves takes 16 rows of a group and 8 / KS tile rows of weights; KS waves share the reduction of a
+// tile row and their sums meet in LDS.  UP: four tile rows make a block of 32 neurons (two of W1, the same two of W3).
 template <bool UP, int KS>
-__global__ __launch_bounds__(64 * kStreamWaves, 2) void mx_stream_kernel(MxArgs a, int cb_r, int cb_s, int rows_cap) {
+__global__ __launch_bounds__(kStreamThreads, 4) void mx_stream_kernel(MxArgs a, int cb_r, int cb_s, int rows_cap) {
     constexpr int NT = kStreamWaves / KS;
     extern __shared__ __align__(16) uint8_t lds[];
     v4f* red = reinterpret_cast<v4f*>(lds);                       // [8 waves][64 lanes]
-    uint8_t* xl = lds + kStreamWaves * 64 * sizeof(v4f);
+    uint8_t* xl = lds + kStreamThreads * sizeof(v4f);
     const MxItem it = mx_find_item<16, false>(a, cb_r, cb_s, (int)blockIdx.x);
     if (it.group < 0) return;
     const bool shared = it.group >= a.E;
-    const int Kp = shared ? a.Kp_s : a.Kp_r;
-    uint8_t* sl = xl + rows_cap * (Kp + 16);
-    MxMatrix m;
-    const bool ok = mx_matrix<UP>(a, it.group, &m);
     const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int tile = wave / KS, ks = wave % KS;
     const long long out0 = shared ? (long long)(it.group - a.E) * a.N + it.row0 : it.row0;   // first output row
-    if (!ok) {
+    const MxSide sd = mx_side(a, shared);
+    const bool y_fp32 = a.y_fp32, y_vec = a.y_vec;
+    MxRowStage rows;
+    rows.Kp = sd.Kp;
+    rows.x = sd.x;
+    rows.xs = sd.xs;
+    rows.k = a.k;
+    rows.rows = it.rows;
+    rows.per_row = rows.Kp / 16;
+    rows.pieces = it.rows * rows.per_row;
+    // (one token: every pair's row is row 0, and the permutation need not be waited for)
+    rows.perm = !shared && a.gather && a.N > 1 ? a.perm : nullptr;
+    rows.first = !a.gather ? out0 : shared || a.N > 1 ? it.row0 : 0;
+    const int row_step = !shared && a.gather && a.N == 1 ? 0 : 1;
+    if (row_step == 0) rows.pieces = rows.per_row;                // all rows of the group are that one
+    uint8_t* sl = xl + rows_cap * (rows.Kp + 16);
+    rows.begin();
+    MxMatrix m;
+    if (!mx_matrix<UP>(a, it.group, &m)) {
         if (!UP && ks == 0 && (lane & 15) < it.rows) {
             const int r0 = (it.col * NT + tile) * 16 + 4 * g;
-            const int cols = shared ? a.cols_s : a.cols_r;
-            mx_store_y(a, shared ? a.y_s : a.y_r, (out0 + (lane & 15)) * (shared ? a.ld_s : a.ld_r) + r0, cols - r0,
-                       v4f{0.0f, 0.0f, 0.0f, 0.0f});
+            if (r0 < sd.cols)
+                mx_store_y(y_fp32, y_vec, sd.y, (out0 + (lane & 15)) * sd.ld + r0, sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
         }
         return;
     }
-    auto stage = [&]() {
-        const uint8_t* xb = shared ? a.x_s : a.x_r;
-        const uint8_t* xsb = shared ? a.xs_s : a.xs_r;
-        const int per_row = Kp / 16, pieces = it.rows * per_row;
-        for (int q = (int)threadIdx.x; q < pieces; q += 64 * kStreamWaves) {
-            const int r = q / per_row, c = q - r * per_row;
-            const long long src = shared ? (a.gather ? it.row0 + r : out0 + r)
-                                         : (a.gather ? a.perm[it.row0 + r] / a.k : it.row0 + r);
-            *reinterpret_cast<v4i*>(xl + r * (Kp + 16) + 16 * c) = reinterpret_cast<const v4i*>(xb + src * Kp)[c];
-            if ((c & 7) == 0)
-                *reinterpret_cast<uint32_t*>(sl + r * (Kp / 32) + c / 2) =
-                    reinterpret_cast<const uint32_t*>(xsb + src * (Kp / 32))[c / 8];
-        }
-        __syncthreads();
-    };
+    if (row_step == 0) rows.rows = 1;                             // (what the waves read, not what is stored)
     const int last = mx_row_tiles(m.rows) - 1;
-    int rb = UP ? it.col * 2 + (tile & 1) : it.col * NT + tile;
+    int rb = UP ? (it.col * (NT / 4) + tile / 4) * 2 + (tile & 1) : it.col * NT + tile;
     rb = rb < last ? rb : last;
-    const bool third = UP && tile >= 2;
+    const bool third = UP && (tile & 2);
     const uint8_t* w = (third ? m.w3 : m.w) + (long long)rb * m.KT * (m.bits == 4 ? 1024 : 2048);
     const uint8_t* ws = (third ? m.s3 : m.s) + (long long)rb * m.KG * 256;
     const int s0 = m.KT * ks / KS, s1 = m.KT * (ks + 1) / KS;
     v4f acc;
-    if (m.bits == 4) acc = stream_tiles<4>(w, ws, s0, s1, Kp, xl, sl, it.rows, stage);
-    else acc = stream_tiles<8>(w, ws, s0, s1, Kp, xl, sl, it.rows, stage);
+    if (m.bits == 4) acc = stream_tiles<4>(w, ws, s0, s1, rows, xl, sl);
+    else acc = stream_tiles<8>(w, ws, s0, s1, rows, xl, sl);
     if constexpr (KS > 1 || UP) {
         red[wave * 64 + lane] = acc;
         __syncthreads();
     }
     if constexpr (UP) {
-        if (wave != 0) return;
+        if (wave % (4 * KS) != 0) return;
         v4f v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[i] = red[i * KS * 64 + lane];
+            v[i] = red[(wave + i * KS) * 64 + lane];
 #pragma unroll
-            for (int p = 1; p < KS; ++p) v[i] += red[(i * KS + p) * 64 + lane];
+            for (int p = 1; p < KS; ++p) v[i] += red[(wave + i * KS + p) * 64 + lane];
         }
-        const int n0 = it.col * 32;
+        const int n0 = (it.col * (NT / 4) + tile / 4) * 32;
         v4f h0, h1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -127,21 +169,20 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void mx_stream_kernel(MxArgs 
             h0[i] = zero ? 0.0f : mx_swiglu(v[0][i], v[2][i]);
             h1[i] = zero ? 0.0f : mx_swiglu(v[1][i], v[3][i]);
         }
-        const long long row = out0 + (lane & 15), ld = shared ? a.ld_s : a.ld_r;
-        mx_store_h(h0, h1, (lane & 15) < it.rows, static_cast<uint8_t*>(shared ? a.y_s : a.y_r) + row * ld + n0,
-                   (shared ? a.ys_s : a.ys_r) + row * (ld / 32) + n0 / 32);
+        const long long row = out0 + (lane & 15);
+        mx_store_h(h0, h1, (lane & 15) < it.rows, static_cast<uint8_t*>(sd.y) + row * sd.ld + n0,
+                   sd.ys + row * (sd.ld / 32) + n0 / 32);
     } else {
         if (ks != 0) return;
 #pragma unroll
         for (int p = 1; p < KS; ++p) acc += red[(wave + p) * 64 + lane];
         const int r0 = (it.col * NT + tile) * 16 + 4 * g;
-        const int cols = shared ? a.cols_s : a.cols_r;
-        if ((lane & 15) < it.rows && r0 < cols) {
+        if ((lane & 15) < it.rows && r0 < sd.cols) {
             if (a.bias != nullptr) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i] += r0 + i < cols ? a.bias[r0 + i] : 0.0f;
+                for (int i = 0; i < 4; ++i) acc[i] += r0 + i < sd.cols ? ld_global<float>(a.bias, r0 + i) : 0.0f;
             }
-            mx_store_y(a, shared ? a.y_s : a.y_r, (out0 + (lane & 15)) * (shared ? a.ld_s : a.ld_r) + r0, cols - r0, acc);
+            mx_store_y(y_fp32, y_vec, sd.y, (out0 + (lane & 15)) * sd.ld + r0, sd.cols - r0, acc);
         }
     }
 }
@@ -202,14 +243,15 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
     const uint8_t* w = a.m.w + (long long)rb * KT * MxWTile<BITS>::kBytes;
     const uint32_t* wsd = reinterpret_cast<const uint32_t*>(a.m.s + (long long)rb * a.m.KG * 256) + lane;
     const int s0 = KT * ks / KS, s1 = KT * (ks + 1) / KS, n = s1 - s0;
-    MxWTile<BITS> wt[kStreamRing];
-    uint32_t sc[kStreamRing];
+    constexpr int R = 8;
+    MxWTile<BITS> wt[R];
+    uint32_t sc[R];
     if (n > 0) {
 #pragma unroll
-        for (int j = 0; j < kStreamRing; ++j) {
+        for (int j = 0; j < R; ++j) {
             const int s = s0 + (j < n ? j : n - 1);
             wt[j].load(w + (long long)s * MxWTile<BITS>::kBytes, lane);
-            sc[j] = wsd[(s >> 2) * 64];
+            sc[j] = ld_global<uint32_t>(wsd, (s >> 2) * 64);
         }
     }
     const int per_row = KT * 16, pieces = rows * per_row;         // of eight elements
@@ -232,10 +274,10 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
     if (n > 0) {
         const int row = (lane & 15) < rows ? lane & 15 : 0;
         const uint16_t* xr = xl + row * ldx + (BITS == 4 ? 32 : 16) * g;
-        for (int base = s0;; base += kStreamRing) {
-            const bool more = base + kStreamRing < s1;
+        for (int base = s0;; base += R) {
+            const bool more = base + R < s1;
 #pragma unroll
-            for (int j = 0; j < kStreamRing; ++j) {
+            for (int j = 0; j < R; ++j) {
                 const int s = base + j;
                 if (s < s1) {
                     // the lane's codes all belong to one row; 8-bit ones to two blocks of it
@@ -255,9 +297,9 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
                     }
                 }
                 if (more) {
-                    const int t = s + kStreamRing < s1 ? s + kStreamRing : s1 - 1;
+                    const int t = s + R < s1 ? s + R : s1 - 1;
                     wt[j].load(w + (long long)t * MxWTile<BITS>::kBytes, lane);
-                    sc[j] = wsd[(t >> 2) * 64];
+                    sc[j] = ld_global<uint32_t>(wsd, (t >> 2) * 64);
                 }
             }
             if (!more) break;
@@ -276,10 +318,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += r0 + i < a.R ? a.bias[r0 + i] : 0.0f;
         }
-        MxArgs o{};
-        o.y_fp32 = a.y_fp32;
-        o.y_vec = a.y_vec;
-        mx_store_y(o, a.y, (t0 + (lane & 15)) * a.ld_y + r0, a.R - r0, acc);
+        mx_store_y(a.y_fp32, a.y_vec, a.y, (t0 + (lane & 15)) * a.ld_y + r0, a.R - r0, acc);
     }
 }
 
@@ -293,10 +332,11 @@ static fate_status allow_lds(F kernel, size_t bytes) {
     return FATE_OK;
 }
 
-// How many waves share a reduction: as few as leave about two workgroups per compute unit, each with two steps or more.
+// How many waves share a reduction: as many as leave all workgroups on the device at once (a workgroup's time is a chain
+// of round trips more than anything else, a second round doubles it), each with two steps or more.
 int mx_k_split(long long tiles, int KT) {
     int ks = 1;
-    while (ks < 8 && tiles * ks / 8 < 512 && KT >= 4 * ks) ks *= 2;
+    while (ks < 8 && tiles * ks * 2 <= 512 * kStreamWaves && KT >= 4 * ks) ks *= 2;
     return ks;
 }
 
@@ -325,7 +365,10 @@ fate_status launch_mx_stream(hipStream_t st, const MxArgs& a, bool up, int rows_
         FATE_HIP(hipGetLastError());
         return FATE_OK;
     };
-    if (up) return go(mx_stream_kernel<true, 2>, 32);
+    if (up) {
+        const long long blocks = tr * (a.cols_r / 32) + ts * (a.cols_s / 32);
+        return blocks <= 768 ? go(mx_stream_kernel<true, 2>, 32) : go(mx_stream_kernel<true, 1>, 64);
+    }
     const int KT = Kp / kMxStep;
     const int ks = mx_k_split(tr * ((a.cols_r + 15) / 16) + ts * ((a.cols_s + 15) / 16), KT);
     switch (ks) {

@@ -1,63 +1,61 @@
-// Products with block-scaled weights for many rows: rows travel memory -> LDS in a ring of stages, weights memory ->
-// registers, both as the matrix instruction takes them.
+// Products with block-scaled weights for many rows: rows go through LDS, weights from memory into registers, both as the
+// matrix instruction takes them.
 #include <type_traits>
 #include "async_lds.h"
 #include "mx_gemm.h"
 
 namespace fate {
 
-constexpr int kTileStages = 4;
-
-// 16 bytes per lane from the lane's own address to lds + lane * 16.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_load16_at(uint32_t lds, const void* vaddr) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(vaddr) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 // A workgroup of four waves multiplies up to RT rows with 256 rows of weights, 64 (four tile rows) per wave; UP: 32 of W1
 // and the same 32 of W3, so that a wave holds what SwiGLU and the block's scale need.
-// Rows lie in LDS as [RT][8 pieces of 16 columns], piece c of row r at place c ^ (r & 7): the 16 lanes that read one
-// piece of 16 rows at a time find them on different banks.
+//
+// Weights are read by one wave each, so they go straight into registers, D steps of 128 columns ahead.  Rows are read by
+// all four: they are loaded up to two steps ahead into registers and lie in LDS one step ahead, [2][RT][8 pieces of 16 columns],
+// piece c of row r at place c ^ (r & 7), so that the 16 lanes that read one piece of 16 rows find them on different banks.
+// All loads are the compiler's own, whose waits count them: loads straight into LDS would have to be counted by hand, and
+// a wait for one of them would also wait for the weights that were requested before it.
 template <int RT, bool UP, int BITS>
 __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, const MxMatrix& m, uint8_t* lds) {
     constexpr int NT = RT / 16;                                   // row tiles of 16
-    constexpr int NL = RT >= 32 ? RT / 32 : 1;                    // loads of rows per wave and stage
-    constexpr int LPS = NL + 1;
+    constexpr int NL = RT >= 32 ? RT / 32 : 1;                    // pieces of 16 bytes of the rows per thread and step
     constexpr int D = RT >= 128 || BITS == 8 ? 2 : 4;             // weight tiles in flight per tile row
+    constexpr int XD = RT >= 128 ? 1 : 2;                         // steps of rows in registers (128: 256 registers are full)
     const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const bool shared = it.group >= a.E;
-    const int Kp = shared ? a.Kp_s : a.Kp_r, KT = m.KT;
+    const MxSide sd = mx_side(a, shared);
+    const int Kp = sd.Kp, KT = m.KT;
     const long long out0 = shared ? (long long)(it.group - a.E) * a.N + it.row0 : it.row0;
-    uint8_t* xl = lds;                                            // [stages][RT * 128]
-    uint8_t* sl = lds + kTileStages * RT * kMxStep;               // [stages][RT * 4]
+    uint8_t* xl = lds;                                            // [2][RT * 128]
+    uint8_t* sl = lds + 2 * RT * kMxStep;                         // [2][RT * 4]
     auto source = [&](int r) -> long long {
         r = r < it.rows ? r : 0;
         if (shared) return a.gather ? it.row0 + r : out0 + r;
-        return a.gather ? a.perm[it.row0 + r] / a.k : it.row0 + r;
+        return a.gather ? ld_global<int>(a.perm, it.row0 + r) / a.k : it.row0 + r;
     };
+    // thread t moves piece t & 7 of rows t / 8, t / 8 + 32, ... and, of its first RT threads, the scales of row t
     const uint8_t* xp[NL];
-    constexpr int kPer = RT * 8 / 4;                              // pieces per wave
+    const int tr = (int)threadIdx.x >> 3, tc = (int)threadIdx.x & 7;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        const int q = wave * kPer + i * 64 + (lane < kPer ? lane : 0);
-        const int r = q >> 3, c = (q & 7) ^ (r & 7);
-        xp[i] = (shared ? a.x_s : a.x_r) + source(r) * Kp + c * 16;
-    }
-    const uint8_t* sp = (shared ? a.xs_s : a.xs_r) + source(wave * (RT / 4) + (lane & (RT / 4 - 1))) * (Kp / 32);
-    const uint32_t xl0 = lds_offset(xl) + wave * kPer * 16, sl0 = lds_offset(sl) + wave * RT;
-    auto issue = [&](int s) {
-        const uint32_t st = (uint32_t)(s & (kTileStages - 1));
+    for (int i = 0; i < NL; ++i) xp[i] = sd.x + source(tr + i * 32) * Kp + tc * 16;
+    const uint8_t* sp = sd.xs + source((int)threadIdx.x & (RT - 1)) * (Kp / 32);
+    const int put = tr * kMxStep + (tc ^ (tr & 7)) * 16;          // (32 rows further the place is the same)
+    const bool put_rows = RT >= 32 || (int)threadIdx.x < RT * 8, put_scale = (int)threadIdx.x < RT;
+    v4i xq[XD][NL];
+    uint32_t sq[XD];
+    auto request = [&](int slot, int s) {
+        s = s < KT ? s : KT - 1;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            if (kPer >= 64 || lane < kPer) lds_load16_at(xl0 + st * (RT * kMxStep) + i * 1024, xp[i] + s * kMxStep);
-        }
-        if (lane < RT / 4) lds_load4(sl0 + st * (RT * 4), sp + s * 4);
+        for (int i = 0; i < NL; ++i) xq[slot][i] = ld_global<v4i>(xp[i] + s * kMxStep);
+        sq[slot] = ld_global<uint32_t>(sp + s * 4);
     };
-    issue(0);
-    if (KT > 1) issue(1);
-    if (KT > 2) issue(2);
+    auto deposit = [&](int slot, int half) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+            if (put_rows) *reinterpret_cast<v4i*>(xl + half * (RT * kMxStep) + put + i * 32 * kMxStep) = xq[slot][i];
+        if (put_scale) reinterpret_cast<uint32_t*>(sl + half * (RT * 4))[threadIdx.x] = sq[slot];
+    };
+    request(0, 0);
+    if constexpr (XD == 2) request(1, 1);
 
     const int last = mx_row_tiles(m.rows) - 1;
     const uint8_t* w[4];
@@ -72,7 +70,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
     MxWTile<BITS> wt[D][4];
     uint32_t sc[4], sn[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sn[i] = ws[i][0];
+    for (int i = 0; i < 4; ++i) sn[i] = ld_global<uint32_t>(ws[i]);
 #pragma unroll
     for (int d = 0; d < D; ++d)
 #pragma unroll
@@ -88,22 +86,22 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
     const uint8_t* xr = xl + (lane & 15) * kMxStep;
     const int c0 = (g ^ (lane & 7)) * 16, c1 = ((4 + g) ^ (lane & 7)) * 16;
     const uint8_t* sr = sl + (lane & 15) * 4 + g;
+    deposit(0, 0);
 
     for (int kg = 0; kg < m.KG; ++kg) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             sc[i] = sn[i];
-            sn[i] = ws[i][(kg + 1 < m.KG ? kg + 1 : kg) * 64];
+            sn[i] = ld_global<uint32_t>(ws[i], (kg + 1 < m.KG ? kg + 1 : kg) * 64);
         }
         auto step = [&](auto J) {
             constexpr int j = decltype(J)::value;
             const int s = kg * 4 + j;
+            lds_only_barrier();                                   // step s lies in LDS, step s - 1 has been read
+            request(j % XD, s + XD);
             if (s < KT) {
-                wait_stages<LPS, 2>(KT - 1 - s);                  // stage s has landed (this wave's part of it)
-                lds_only_barrier();                               // everyone's part; stage s - 1 is read
-                if (s + 3 < KT) issue(s + 3);
-                const uint8_t* xs = xr + j * (RT * kMxStep);
-                const uint8_t* ss = sr + j * (RT * 4);
+                const uint8_t* xs = xr + (j & 1) * (RT * kMxStep);
+                const uint8_t* ss = sr + (j & 1) * (RT * 4);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const v4i lo = *reinterpret_cast<const v4i*>(xs + t * 16 * kMxStep + c0);
@@ -113,10 +111,11 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[t][i] = wt[j % D][i].template mfma<j>(sc[i], x, e, acc[t][i]);
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    wt[j % D][i].load(w[i] + (long long)(s + D < KT ? s + D : KT - 1) * MxWTile<BITS>::kBytes, lane);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                wt[j % D][i].load(w[i] + (long long)(s + D < KT ? s + D : KT - 1) * MxWTile<BITS>::kBytes, lane);
+            deposit((j + 1) % XD, (j + 1) & 1);                   // step s + 1
         };
         step(std::integral_constant<int, 0>{});
         step(std::integral_constant<int, 1>{});
@@ -124,12 +123,11 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
         step(std::integral_constant<int, 3>{});
     }
 
-    const long long ld = shared ? a.ld_s : a.ld_r;
+    const long long ld = sd.ld;
     if constexpr (UP) {
         const int n0 = it.col * 128 + wave * 32;
         const bool zero = n0 >= m.rows;                           // padding columns of h
-        uint8_t* y = static_cast<uint8_t*>(shared ? a.y_s : a.y_r);
-        uint8_t* ys = shared ? a.ys_s : a.ys_r;
+        uint8_t* y = static_cast<uint8_t*>(sd.y);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int r = t * 16 + (lane & 15);
@@ -140,11 +138,11 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
                 h1[i] = zero ? 0.0f : mx_swiglu(acc[t][1][i], acc[t][3][i]);
             }
             const long long row = out0 + r;
-            mx_store_h(h0, h1, r < it.rows, y + row * ld + n0, ys + row * (ld / 32) + n0 / 32);
+            mx_store_h(h0, h1, r < it.rows, y + row * ld + n0, sd.ys + row * (ld / 32) + n0 / 32);
         }
     } else {
-        const int cols = shared ? a.cols_s : a.cols_r;
-        void* y = shared ? a.y_s : a.y_r;
+        const int cols = sd.cols;
+        const bool y_fp32 = a.y_fp32, y_vec = a.y_vec;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int r = t * 16 + (lane & 15);
@@ -156,9 +154,9 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
                         v4f v = acc[t][i];
                         if (a.bias != nullptr) {
 #pragma unroll
-                            for (int b = 0; b < 4; ++b) v[b] += r0 + b < cols ? a.bias[r0 + b] : 0.0f;
+                            for (int b = 0; b < 4; ++b) v[b] += r0 + b < cols ? ld_global<float>(a.bias, r0 + b) : 0.0f;
                         }
-                        mx_store_y(a, y, (out0 + r) * ld + r0, cols - r0, v);
+                        mx_store_y(y_fp32, y_vec, sd.y, (out0 + r) * ld + r0, cols - r0, v);
                     }
                 }
             }
@@ -187,13 +185,12 @@ __global__ __launch_bounds__(256, 2) void mx_tile_kernel(MxArgs a, int cb_r, int
     if (!mx_matrix<UP>(a, it.group, &m)) {
         if constexpr (!UP) {                                      // an expert that cannot be used adds nothing
             const bool shared = it.group >= a.E;
-            const int cols = shared ? a.cols_s : a.cols_r;
+            const MxSide sd = mx_side(a, shared);
             const long long out0 = shared ? (long long)(it.group - a.E) * a.N + it.row0 : it.row0;
             for (int q = (int)threadIdx.x; q < it.rows * 64; q += 256) {
                 const int r = q >> 6, r0 = it.col * 256 + (q & 63) * 4;
-                if (r0 < cols)
-                    mx_store_y(a, shared ? a.y_s : a.y_r, (out0 + r) * (shared ? a.ld_s : a.ld_r) + r0, cols - r0,
-                               v4f{0.0f, 0.0f, 0.0f, 0.0f});
+                if (r0 < sd.cols)
+                    mx_store_y(a.y_fp32, a.y_vec, sd.y, (out0 + r) * sd.ld + r0, sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
             }
         }
         return;
@@ -211,10 +208,7 @@ static fate_status launch_tile(hipStream_t st, const MxArgs& a) {
     const long long items = mx_max_tiles(a, RT) * cb_r + (long long)a.n_shared * ((a.N + RT - 1) / RT) * cb_s;
     const long long grid = (items + 7) / 8 * 8;
     if (grid > 0x7fffffffLL) FATE_FAIL(FATE_ESHAPE, "too many workgroups (%lld)", grid);
-    const size_t lds = (size_t)kTileStages * RT * (kMxStep + 4);
-    if (lds > 64 * 1024)
-        FATE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(mx_tile_kernel<RT, UP>),
-                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    const size_t lds = (size_t)2 * RT * (kMxStep + 4);
     mx_tile_kernel<RT, UP><<<(unsigned)grid, 256, lds, st>>>(a, cb_r, cb_s);
     FATE_HIP(hipGetLastError());
     return FATE_OK;
