@@ -415,7 +415,8 @@ fate_status fate_mx_linear(void* stream, int N, int K, int R, const void* x, int
  * multiples of 32, mode 0.  An activated expert whose w1 is NULL is flagged in
  * the int32 at workspace offset 0 (bit 0) and contributes nothing, as does (bit 2)
  * an entry of another format.  Sums as in fate_mx_linear; the rows of the down
- * product are kept in y's type until they are added up in fp32.
+ * product (of long reductions: of parts of it) are kept in fp32, or, for more than
+ * a few tokens, in y's type until they are added up in fp32.
  * workspace: what calls of up to N tokens need; calls that share one are ordered
  * on one stream.
  * ---------------------------------------------------------------------- */

@@ -326,41 +326,50 @@ _TYPE_OF = {torch.bfloat16: FATE_BF16, torch.float32: FATE_FP32}
 MX_GROUP = 32
 
 
-def _need(cond, msg):
-    if not cond:
-        raise FateError(1, msg)
+def _refuse(msg):
+    raise FateError(1, msg)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _rows(t, name, shape=None):
-    """(type, distance between rows) of a matrix whose rows are contiguous."""
-    _need(t.dim() == 2 and t.dtype in _TYPE_OF, f"{name} is a matrix of bf16 or fp32")
-    _need(shape is None or t.shape == shape, f"{name} is {tuple(t.shape)}, {tuple(shape or ())} expected")
-    _need(t.stride(1) == 1 or t.shape[1] == 1, f"the rows of {name} are not contiguous")
-    # (a single row has no distance, whatever its stride says)
-    return _TYPE_OF[t.dtype], max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+# (The checks run on every call, between kernels of a few microseconds: messages are put together only when needed.)
+def _rows(t, name, shape):
+    """(type, distance between rows) of a matrix of that shape whose rows are contiguous."""
+    if t.shape != shape or len(shape) != 2:
+        _refuse(f"{name} is {tuple(t.shape)}, a matrix {tuple(shape)} expected")
+    kind = _TYPE_OF.get(t.dtype)
+    if kind is None:
+        _refuse(f"{name} is a matrix of bf16 or fp32")
+    ld, step = t.stride()
+    if step != 1 and shape[1] != 1:
+        _refuse(f"the rows of {name} are not contiguous")
+    # (a single row has no distance, whatever its stride says; rows that overlap are refused by the library)
+    return kind, ld if shape[0] > 1 else shape[1]
 
 
 def _dense(t, name, dtype, shape):
-    _need(t.dtype == dtype and t.shape == shape and t.is_contiguous(), f"{name} is a contiguous {dtype} tensor {tuple(shape)}")
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} is a contiguous {dtype} tensor {tuple(shape)}")
 
 
 def _here(stream, *tensors):
     """The stream to launch on: tensors of a launch live on the current device, which owns the stream."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != dev:
-            raise FateError(1, f"a tensor on {t.device}, the current device is cuda:{dev}")
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        if t is not None and t.get_device() != dev:
+            _refuse(f"a tensor on {t.device}, the current device is cuda:{dev}")
+    # (torch.cuda.current_stream() builds an object, for longer than a kernel takes)
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _apart(out, *inputs):
-    """Outputs that are their own memory: a full overlap with an input is always a mistake."""
+    """Outputs are memory of their own: one that starts where an input does is always a mistake."""
+    p = out.data_ptr()
     for t in inputs:
-        _need(t is None or out is None or out.data_ptr() != t.data_ptr() or out.numel() == 0, "an output is also an input")
+        if t is not None and t.data_ptr() == p and p:
+            _refuse("an output is also an input")
 
 
 def mx_padded(K):
@@ -375,17 +384,19 @@ def mx_empty(rows, K, device="cuda"):
             torch.empty(rows, Kp // MX_GROUP, dtype=torch.uint8, device=device))
 
 
-def _check_mx(codes, scales, rows, K, name):
-    Kp = mx_padded(K)
-    _dense(codes, f"{name} codes", torch.uint8, (rows, Kp))
-    _dense(scales, f"{name} scales", torch.uint8, (rows, Kp // MX_GROUP))
+def _check_mx(codes, scales, rows, K):
+    Kp = -(-K // 128) * 128
+    if codes.dtype != torch.uint8 or codes.shape != (rows, Kp) or not codes.is_contiguous() or \
+            scales.dtype != torch.uint8 or scales.shape != (rows, Kp // 32) or not scales.is_contiguous():
+        _refuse(f"8-bit rows are contiguous uint8 tensors: codes {(rows, Kp)} and scales {(rows, Kp // 32)}")
 
 
 def fate_mx_quantize(x, codes, scales, stream=None):
-    t, ld = _rows(x, "x")
-    N, K = x.shape
-    _check_mx(codes, scales, N, K, "output")
-    _check(lib().fate_mx_quantize(_here(stream, x, codes, scales), x.data_ptr(), t, N, K, ld, codes.data_ptr(),
+    shape = x.shape
+    kind, ld = _rows(x, "x", shape)
+    N, K = shape
+    _check_mx(codes, scales, N, K)
+    _check(lib().fate_mx_quantize(_here(stream, x, codes, scales), x.data_ptr(), kind, N, K, ld, codes.data_ptr(),
                                   scales.data_ptr()))
 
 
@@ -397,11 +408,12 @@ def fate_mx_weight_bytes(rows, K, bits):
 
 
 def fate_mx_pack_weight(w, bits, codes, scales, stream=None):
-    t, ld = _rows(w, "w")
-    cb, sb = fate_mx_weight_bytes(*w.shape, bits)
+    kind, ld = _rows(w, "w", w.shape)
+    R, K = w.shape
+    cb, sb = fate_mx_weight_bytes(R, K, bits)
     _dense(codes, "codes", torch.uint8, (cb,))
     _dense(scales, "scales", torch.uint8, (sb,))
-    _check(lib().fate_mx_pack_weight(_here(stream, w, codes, scales), w.data_ptr(), t, *w.shape, ld, bits,
+    _check(lib().fate_mx_pack_weight(_here(stream, w, codes, scales), w.data_ptr(), kind, R, K, ld, bits,
                                      codes.data_ptr(), scales.data_ptr()))
 
 
@@ -424,7 +436,8 @@ class MxExpert:
     """One SwiGLU expert of block-scaled matrices W1 [I, H], W3 [I, H], W2 [H, I]."""
 
     def __init__(self, w1, w3, w2):
-        _need(w1.bits == w3.bits == w2.bits and (w1.R, w1.K) == (w3.R, w3.K) == (w2.K, w2.R), "W1, W3 and W2 do not fit")
+        if not (w1.bits == w3.bits == w2.bits and (w1.R, w1.K) == (w3.R, w3.K) == (w2.K, w2.R)):
+            _refuse("W1, W3 and W2 do not fit")
         self.w1, self.w3, self.w2, self.bits, self.group, self.I, self.H = w1, w3, w2, w1.bits, MX_GROUP, w1.R, w1.K
 
     def struct(self):
@@ -439,26 +452,30 @@ class MxExpert:
 def fate_add_rmsnorm(h, delta=None, weight=None, eps=1e-6, h_out=None, x=None, mx=None, stream=None):
     """h [N, H], delta [N, H] or None, weight [H] or None; outputs h_out [N, H] of h's type (may be h), x [N, H] bf16,
     mx = (codes, scales), each of them or None."""
-    N, H = h.shape
-    th, ld_h = _rows(h, "h")
+    shape = h.shape
+    th, ld_h = _rows(h, "h", shape)
+    N, H = shape
     td = ld_d = tw = ld_o = ld_x = 0
     if delta is not None:
-        td, ld_d = _rows(delta, "delta", h.shape)
+        td, ld_d = _rows(delta, "delta", shape)
     if weight is not None:
-        _need(weight.dtype in _TYPE_OF and weight.shape == (H,) and weight.is_contiguous(), "weight is a vector [H] of bf16 or fp32")
-        tw = _TYPE_OF[weight.dtype]
+        tw = _TYPE_OF.get(weight.dtype)
+        if tw is None or weight.shape != (H,) or not weight.is_contiguous():
+            _refuse("weight is a contiguous vector [H] of bf16 or fp32")
     if h_out is not None:
-        to, ld_o = _rows(h_out, "h_out", h.shape)
-        _need(to == th, "h_out has h's type")
+        to, ld_o = _rows(h_out, "h_out", shape)
+        if to != th:
+            _refuse("h_out has h's type")
         _apart(h_out, delta, weight)
     if x is not None:
-        tx, ld_x = _rows(x, "x", h.shape)
-        _need(tx == FATE_BF16, "x is bf16")
+        tx, ld_x = _rows(x, "x", shape)
+        if tx != FATE_BF16:
+            _refuse("x is bf16")
         _apart(x, h, delta, weight, h_out)
     codes = scales = None
     if mx is not None:
         codes, scales = mx
-        _check_mx(codes, scales, N, H, "x")
+        _check_mx(codes, scales, N, H)
     _check(lib().fate_add_rmsnorm(_here(stream, h, delta, weight, h_out, x, codes, scales), N, H, h.data_ptr(), th, ld_h,
                                   _ptr(delta), td, ld_d, _ptr(weight), tw, eps, _ptr(h_out), ld_o, _ptr(x), ld_x,
                                   _ptr(codes), _ptr(scales)))
@@ -466,19 +483,21 @@ def fate_add_rmsnorm(h, delta=None, weight=None, eps=1e-6, h_out=None, x=None, m
 
 def fate_mx_linear(x, w, y, bias=None, stream=None):
     """x: a bf16 matrix [N, K], or 8-bit rows (codes, scales); w: an MxWeight [R, K]; y [N, R] bf16 or fp32."""
-    if isinstance(x, tuple):
+    K, R, xs = w.K, w.R, None
+    if type(x) is tuple:
         x, xs = x
         N, tx, ld_x = x.shape[0], FATE_MXFP8, 0
-        _check_mx(x, xs, N, w.K, "x")
+        _check_mx(x, xs, N, K)
     else:
-        xs, N = None, x.shape[0]
-        tx, ld_x = _rows(x, "x", (N, w.K))
-        _need(tx == FATE_BF16, "x is bf16 or 8-bit rows")
-    ty, ld_y = _rows(y, "y", (N, w.R))
+        N = x.shape[0]
+        tx, ld_x = _rows(x, "x", (N, K))
+        if tx != FATE_BF16:
+            _refuse("x is bf16 or 8-bit rows")
+    ty, ld_y = _rows(y, "y", (N, R))
     if bias is not None:
-        _dense(bias, "bias", torch.float32, (w.R,))
+        _dense(bias, "bias", torch.float32, (R,))
     _apart(y, x, bias)
-    _check(lib().fate_mx_linear(_here(stream, x, xs, w.codes, w.scales, bias, y), N, w.K, w.R, x.data_ptr(), tx, ld_x,
+    _check(lib().fate_mx_linear(_here(stream, x, xs, w.codes, w.scales, bias, y), N, K, R, x.data_ptr(), tx, ld_x,
                                 _ptr(xs), w.bits, w.codes.data_ptr(), w.scales.data_ptr(), _ptr(bias), y.data_ptr(), ty,
                                 ld_y))
 
@@ -491,11 +510,11 @@ def fate_moe_ffn_mx_workspace(desc):
 
 def fate_moe_ffn_mx(desc, x_codes, x_scales, experts_dev, counts, offsets, perm, inv_perm, expert_order, topk_w,
                     shared_dev, shared_gate, y, workspace, stream=None):
-    _check_mx(x_codes, x_scales, desc.N, desc.H, "x")
-    _dense(y, "y", torch.float32 if desc.y_is_fp32 else torch.bfloat16, (desc.N, desc.H))
+    N, H = desc.N, desc.H
+    _check_mx(x_codes, x_scales, N, H)
+    _dense(y, "y", torch.float32 if desc.y_is_fp32 else torch.bfloat16, (N, H))
     _check(lib().fate_moe_ffn_mx(_here(stream, x_codes, x_scales, experts_dev, counts, offsets, perm, inv_perm,
                                        expert_order, topk_w, shared_dev, shared_gate, y, workspace), C.addressof(desc),
                                  x_codes.data_ptr(), x_scales.data_ptr(), _ptr(experts_dev), _ptr(counts), _ptr(offsets),
                                  _ptr(perm), _ptr(inv_perm), _ptr(expert_order), _ptr(topk_w), _ptr(shared_dev),
-                                 _ptr(shared_gate), y.data_ptr(), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size()))
+                                 _ptr(shared_gate), y.data_ptr(), _ptr(workspace), workspace.nbytes))

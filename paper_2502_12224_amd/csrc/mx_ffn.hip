@@ -5,7 +5,9 @@ namespace fate {
 
 int mx_stream_rows(long long rows, int Kp);
 fate_status launch_mx_stream(hipStream_t st, const MxArgs& a, bool up, int rows_cap);
-fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up, long long rows);
+fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up);
+long long mx_tile_items(const MxArgs& a, bool up, int RT);
+int mx_tile_rows(const MxArgs& a, bool up);
 fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x, const MxMatrix& m, const float* bias,
                                   void* y, long long ld_y, int N, int K, int R, int y_fp32, int y_vec);
 
@@ -15,6 +17,8 @@ struct MxCombineArgs {
     const uint8_t* x; const uint8_t* xs; const uint16_t* gate;
     void* y;
     int N, k, H, n_shared, Kp;
+    int parts_r, parts_s;                   // partial sums of a row, `part` elements apart
+    long long part_r, part_s;
 };
 
 template <typename T>
@@ -28,7 +32,7 @@ __device__ __forceinline__ v4f row4(const void* rows, long long at) {
 
 // y[t] = sum_j w[t,j] row[inv_perm[t,j]] + g(t) sum_v shared row: one workgroup per token, terms in the order of j, then v.
 // The rows are requested before the gate is known; what is left is two round trips and the launch.
-template <typename T>
+template <typename T, typename TY>
 __global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
     __shared__ float part[16];
     const long long t = blockIdx.x;
@@ -60,9 +64,13 @@ __global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j0 + j < a.k && (unsigned)s[j] < (unsigned)P) y += w[j] * row4<T>(a.rows_r, (long long)s[j] * a.H + i);
+                    if (j0 + j < a.k && (unsigned)s[j] < (unsigned)P)
+                        for (int p = 0; p < a.parts_r; ++p) y += w[j] * row4<T>(a.rows_r, p * a.part_r + (long long)s[j] * a.H + i);
             }
-            for (int v = 0; v < a.n_shared; ++v) z += row4<T>(a.rows_s, ((long long)v * a.N + t) * a.H + i);
+            for (int v = 0; v < a.n_shared * a.parts_s; ++v) {
+                const int p = v / a.n_shared;
+                z += row4<T>(a.rows_s, p * a.part_s + ((long long)(v - p * a.n_shared) * a.N + t) * a.H + i);
+            }
         }
         if (a.gate != nullptr && i0 == 0) {
             dot = wave_sum(dot);
@@ -74,7 +82,7 @@ __global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
         }
         y += gate * z;
         if (i < a.H) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f*>(static_cast<float*>(a.y) + t * a.H + i) = y;
+            if constexpr (sizeof(TY) == 4) *reinterpret_cast<v4f*>(static_cast<float*>(a.y) + t * a.H + i) = y;
             else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.H + i) =
                      make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
         }
@@ -104,6 +112,8 @@ static fate_status check_mx_desc(const fate_ffn_desc* d) {
     return FATE_OK;
 }
 
+constexpr int kMxMostParts = 4;
+
 struct MxWorkspace {
     size_t h_r, hs_r, h_s, hs_s, rows_r, rows_s, bytes;
 };
@@ -118,22 +128,26 @@ static MxWorkspace mx_workspace(const fate_ffn_desc& d) {
     w.hs_r = off; off += up(P * Ip / kMxBlock);
     w.h_s = off; off += up(S * Is);
     w.hs_s = off; off += up(S * Is / kMxBlock);
-    w.rows_r = off; off += up(P * d.H * (d.y_is_fp32 ? 4 : 2));
-    w.rows_s = off; off += up(S * d.H * (d.y_is_fp32 ? 4 : 2));
+    // (room for two parts of routed rows and the most of shared ones, in bf16 more than one part in fp32: what calls of
+    // up to N tokens need rises with N)
+    w.rows_r = off; off += up(P * d.H * (d.y_is_fp32 ? 4 : 2) * 2);
+    w.rows_s = off; off += up(S * d.H * (d.y_is_fp32 ? 4 : 2) * kMxMostParts);
     w.bytes = off;
     return w;
 }
 
-// Few rows per group, and they fit into LDS: weights are streamed once for 16 rows each; otherwise tiles.
-static fate_status launch_product(hipStream_t st, const MxArgs& a, bool up) {
+// Rows that the streaming kernel keeps in LDS, 0: tiles.  It reads a matrix once for 16 rows, in workgroups of 16 to 128
+// weight rows: for up to 16 tokens, and where tiles of 256 weight rows would leave most of the device idle (streamed /
+// tiles, us: product of 64 x 2048 x 2048 7.8 / 10.8, of 64 x 4096 x 4096 13.3 / 13.9, of 128 x 4096 x 4096 17.0 / 14.9).
+static int stream_rows(const MxArgs& a, bool up) {
     const long long P = (long long)a.N * a.k;
-    const long long cap_rows = a.E && P > a.N ? P : a.N;
-    const int Kp = a.Kp_r > a.Kp_s ? a.Kp_r : a.Kp_s;
-    const int cap = mx_stream_rows(cap_rows, Kp);
-    const long long groups = a.E ? (P < a.E ? P : a.E) : 1;
-    const long long rows = a.E ? (P + groups - 1) / groups : a.N;
-    if (cap && a.N <= 16) return launch_mx_stream(st, a, up, cap);
-    return launch_mx_tile(st, a, up, rows);
+    if (a.N > 16 && mx_tile_items(a, up, a.E ? 32 : 16) >= 96) return 0;
+    return mx_stream_rows(a.E && P > a.N ? P : a.N, a.Kp_r > a.Kp_s ? a.Kp_r : a.Kp_s);
+}
+
+static fate_status launch_product(hipStream_t st, const MxArgs& a, bool up) {
+    const int rows = stream_rows(a, up);
+    return rows ? launch_mx_stream(st, a, up, rows) : launch_mx_tile(st, a, up);
 }
 
 }  // namespace fate
@@ -171,6 +185,7 @@ extern "C" fate_status fate_mx_linear(void* stream, int N, int K, int R, const v
     a.x_s = static_cast<const uint8_t*>(x); a.xs_s = static_cast<const uint8_t*>(x_scales); a.Kp_s = mx_padded(K);
     a.y_s = y; a.ld_s = ld_y; a.cols_s = R; a.K_s = K;
     a.down = 1; a.y_fp32 = y_fp32; a.y_vec = y_vec; a.bias = bias;
+    a.parts_r = a.parts_s = 1;
     return launch_product(st, a, false);
 }
 
@@ -227,16 +242,31 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     a.Kp_s = d->n_shared ? mx_padded(d->I_shared_max) : 0; a.K_s = d->I_shared_max;
     a.y_r = base + w.rows_r; a.y_s = base + w.rows_s;
     a.ld_r = a.ld_s = a.cols_r = a.cols_s = d->H;
-    a.y_fp32 = d->y_is_fp32; a.y_vec = 1;
+    a.y_vec = 1;
+    a.parts_r = a.parts_s = 1;
+    a.part_r = (long long)d->N * d->k * d->H;
+    a.part_s = (long long)d->N * d->n_shared * d->H;
+    const bool streamed = stream_rows(a, false) != 0;
+    a.y_fp32 = d->y_is_fp32 || streamed;                          // (few rows: their bytes do not count)
+    if (!streamed) {
+        // a shared expert's reduction may be several times as long as a routed one's: parts of about that length
+        // (Qwen shape, 4 parts: 512 tokens 126 -> 107 us, 2048 tokens 276 -> 228)
+        const int kr = mx_steps(d->I_max), ks = d->n_shared ? mx_steps(d->I_shared_max) : 0;
+        a.parts_s = ks > kr ? (ks + kr / 2) / kr : 1;
+        if (a.parts_s > kMxMostParts) a.parts_s = kMxMostParts;
+        // fewer workgroups than half the device holds: two parts (Mixtral shape, 256 tokens: 220 -> 186 us)
+        if (mx_tile_items(a, false, mx_tile_rows(a, false)) <= 192 && mx_step_groups(d->I_max) >= 8) a.parts_r = 2;
+    }
     s = launch_product(st, a, false);
     if (s != FATE_OK) return s;
 
     MxCombineArgs c{base + w.rows_r, base + w.rows_s, inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
                     static_cast<const uint8_t*>(x_scales), d->n_shared ? static_cast<const uint16_t*>(shared_gate_bf16) : nullptr,
-                    y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H)};
+                    y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H), a.parts_r, a.parts_s, a.part_r, a.part_s};
     const int threads = d->H >= 4096 ? 1024 : (d->H + 255) / 256 * 64;
-    if (d->y_is_fp32) mx_combine_kernel<float><<<d->N, threads, 0, st>>>(c);
-    else mx_combine_kernel<uint16_t><<<d->N, threads, 0, st>>>(c);
+    if (d->y_is_fp32) mx_combine_kernel<float, float><<<d->N, threads, 0, st>>>(c);
+    else if (a.y_fp32) mx_combine_kernel<float, uint16_t><<<d->N, threads, 0, st>>>(c);
+    else mx_combine_kernel<uint16_t, uint16_t><<<d->N, threads, 0, st>>>(c);
     FATE_HIP(hipGetLastError());
     return FATE_OK;
 }

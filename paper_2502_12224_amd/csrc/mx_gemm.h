@@ -28,6 +28,9 @@ struct MxArgs {
     void* y_s; uint8_t* ys_s; long long ld_s;
     int cols_r, cols_s;                     // output columns (UP: padded to 128)
     int K_r, K_s;                           // nominal reduction lengths (I of an entry may be smaller)
+    // parts that a reduction is cut into (tile kernel, not UP): part p of a row is written `part` elements further each
+    int parts_r, parts_s;
+    long long part_r, part_s;
     int down;                               // entries' w2 with K = I; otherwise w1 (and w3) with K = H
     int y_fp32, y_vec;                      // output type; rows allow 4-wide stores
     const float* bias;
@@ -53,13 +56,13 @@ __device__ __forceinline__ T pick(bool c, T a, T b) { return c ? a : b; }
 struct MxSide {
     const uint8_t* x; const uint8_t* xs;
     void* y; uint8_t* ys;
-    long long ld;
-    int Kp, cols;
+    long long ld, part;
+    int Kp, cols, parts;
 };
 __device__ __forceinline__ MxSide mx_side(const MxArgs& a, bool shared) {
     return MxSide{pick(shared, a.x_s, a.x_r), pick(shared, a.xs_s, a.xs_r), pick(shared, a.y_s, a.y_r),
-                  pick(shared, a.ys_s, a.ys_r), pick(shared, a.ld_s, a.ld_r), pick(shared, a.Kp_s, a.Kp_r),
-                  pick(shared, a.cols_s, a.cols_r)};
+                  pick(shared, a.ys_s, a.ys_r), pick(shared, a.ld_s, a.ld_r), pick(shared, a.part_s, a.part_r),
+                  pick(shared, a.Kp_s, a.Kp_r), pick(shared, a.cols_s, a.cols_r), pick(shared, a.parts_s, a.parts_r)};
 }
 
 // The piece of work number `item`: shared groups first (their reductions are the long ones), then the experts; within

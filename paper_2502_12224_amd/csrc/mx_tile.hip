@@ -14,16 +14,20 @@ namespace fate {
 // piece c of row r at place c ^ (r & 7), so that the 16 lanes that read one piece of 16 rows find them on different banks.
 // All loads are the compiler's own, whose waits count them: loads straight into LDS would have to be counted by hand, and
 // a wait for one of them would also wait for the weights that were requested before it.
+// PLAIN: the reduction may be cut into parts of whole scale dwords (four steps).
 template <int RT, bool UP, int BITS>
-__device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, const MxMatrix& m, uint8_t* lds) {
+__device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, int part, const MxMatrix& m, uint8_t* lds) {
     constexpr int NT = RT / 16;                                   // row tiles of 16
     constexpr int NL = RT >= 32 ? RT / 32 : 1;                    // pieces of 16 bytes of the rows per thread and step
-    constexpr int D = RT >= 128 || BITS == 8 ? 2 : 4;             // weight tiles in flight per tile row
+    constexpr int D = BITS == 8 ? (RT >= 128 ? 2 : 1) : RT >= 64 ? 2 : 4;   // weight tiles in flight per tile row
     constexpr int XD = RT >= 128 ? 1 : 2;                         // steps of rows in registers (128: 256 registers are full)
     const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const bool shared = it.group >= a.E;
     const MxSide sd = mx_side(a, shared);
-    const int Kp = sd.Kp, KT = m.KT;
+    const int Kp = sd.Kp;
+    const int kg0 = UP ? 0 : m.KG * part / sd.parts, kg1 = UP ? m.KG : m.KG * (part + 1) / sd.parts;
+    const int s0 = kg0 * 4, KT = kg1 * 4 < m.KT ? kg1 * 4 : m.KT; // the steps s0 .. KT - 1 (none: the sums stay zero)
+    const int end = KT > s0 ? KT - 1 : s0 < m.KT ? s0 : m.KT - 1; // loads stay at it
     const long long out0 = shared ? (long long)(it.group - a.E) * a.N + it.row0 : it.row0;
     uint8_t* xl = lds;                                            // [2][RT * 128]
     uint8_t* sl = lds + 2 * RT * kMxStep;                         // [2][RT * 4]
@@ -43,7 +47,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
     v4i xq[XD][NL];
     uint32_t sq[XD];
     auto request = [&](int slot, int s) {
-        s = s < KT ? s : KT - 1;
+        s = s < end ? s : end;
 #pragma unroll
         for (int i = 0; i < NL; ++i) xq[slot][i] = ld_global<v4i>(xp[i] + s * kMxStep);
         sq[slot] = ld_global<uint32_t>(sp + s * 4);
@@ -54,8 +58,8 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
             if (put_rows) *reinterpret_cast<v4i*>(xl + half * (RT * kMxStep) + put + i * 32 * kMxStep) = xq[slot][i];
         if (put_scale) reinterpret_cast<uint32_t*>(sl + half * (RT * 4))[threadIdx.x] = sq[slot];
     };
-    request(0, 0);
-    if constexpr (XD == 2) request(1, 1);
+    request(0, s0);
+    if constexpr (XD == 2) request(1, s0 + 1);
 
     const int last = mx_row_tiles(m.rows) - 1;
     const uint8_t* w[4];
@@ -64,18 +68,18 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
     for (int i = 0; i < 4; ++i) {
         int rb = UP ? it.col * 8 + wave * 2 + (i & 1) : it.col * 16 + wave * 4 + i;
         rb = rb < last ? rb : last;
-        w[i] = (UP && i >= 2 ? m.w3 : m.w) + (long long)rb * KT * MxWTile<BITS>::kBytes;
+        w[i] = (UP && i >= 2 ? m.w3 : m.w) + (long long)rb * m.KT * MxWTile<BITS>::kBytes;
         ws[i] = reinterpret_cast<const uint32_t*>((UP && i >= 2 ? m.s3 : m.s) + (long long)rb * m.KG * 256) + lane;
     }
     MxWTile<BITS> wt[D][4];
     uint32_t sc[4], sn[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sn[i] = ld_global<uint32_t>(ws[i]);
+    for (int i = 0; i < 4; ++i) sn[i] = ld_global<uint32_t>(ws[i], (kg0 < m.KG ? kg0 : m.KG - 1) * 64);
 #pragma unroll
     for (int d = 0; d < D; ++d)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            wt[d][i].load(w[i] + (long long)(d < KT ? d : KT - 1) * MxWTile<BITS>::kBytes, lane);
+            wt[d][i].load(w[i] + (long long)(s0 + d < end ? s0 + d : end) * MxWTile<BITS>::kBytes, lane);
 
     v4f acc[NT][4];
 #pragma unroll
@@ -88,11 +92,11 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
     const uint8_t* sr = sl + (lane & 15) * 4 + g;
     deposit(0, 0);
 
-    for (int kg = 0; kg < m.KG; ++kg) {
+    for (int kg = kg0; kg < kg1; ++kg) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             sc[i] = sn[i];
-            sn[i] = ld_global<uint32_t>(ws[i], (kg + 1 < m.KG ? kg + 1 : kg) * 64);
+            sn[i] = ld_global<uint32_t>(ws[i], (kg + 1 < kg1 ? kg + 1 : kg) * 64);
         }
         auto step = [&](auto J) {
             constexpr int j = decltype(J)::value;
@@ -114,7 +118,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                wt[j % D][i].load(w[i] + (long long)(s + D < KT ? s + D : KT - 1) * MxWTile<BITS>::kBytes, lane);
+                wt[j % D][i].load(w[i] + (long long)(s + D < end ? s + D : end) * MxWTile<BITS>::kBytes, lane);
             deposit((j + 1) % XD, (j + 1) & 1);                   // step s + 1
         };
         step(std::integral_constant<int, 0>{});
@@ -152,11 +156,11 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
                     const int r0 = (it.col * 16 + wave * 4 + i) * 16 + 4 * g;
                     if (r0 < cols) {
                         v4f v = acc[t][i];
-                        if (a.bias != nullptr) {
+                        if (a.bias != nullptr && part == 0) {
 #pragma unroll
                             for (int b = 0; b < 4; ++b) v[b] += r0 + b < cols ? ld_global<float>(a.bias, r0 + b) : 0.0f;
                         }
-                        mx_store_y(y_fp32, y_vec, sd.y, (out0 + r) * ld + r0, cols - r0, v);
+                        mx_store_y(y_fp32, y_vec, sd.y, part * sd.part + (out0 + r) * ld + r0, cols - r0, v);
                     }
                 }
             }
@@ -166,21 +170,27 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, con
 
 // A group's last tile, and small groups, take the body for as many rows as they have.
 template <int RT, bool UP, int BITS>
-__device__ __forceinline__ void tile_by_rows(const MxArgs& a, const MxItem& it, const MxMatrix& m, uint8_t* lds) {
+__device__ __forceinline__ void tile_by_rows(const MxArgs& a, const MxItem& it, int part, const MxMatrix& m, uint8_t* lds) {
     if constexpr (RT > 16) {
         if (it.rows <= RT / 2) {
-            tile_by_rows<RT / 2, UP, BITS>(a, it, m, lds);
+            tile_by_rows<RT / 2, UP, BITS>(a, it, part, m, lds);
             return;
         }
     }
-    tile_body<RT, UP, BITS>(a, it, m, lds);
+    tile_body<RT, UP, BITS>(a, it, part, m, lds);
 }
 
 template <int RT, bool UP>
-__global__ __launch_bounds__(256, 2) void mx_tile_kernel(MxArgs a, int cb_r, int cb_s) {
+__global__ __launch_bounds__(256, RT >= 128 ? 2 : 3) void mx_tile_kernel(MxArgs a, int cb_r, int cb_s) {
     extern __shared__ __align__(16) uint8_t lds[];
-    const MxItem it = mx_find_item<RT, true>(a, cb_r, cb_s, (int)blockIdx.x);
+    MxItem it = mx_find_item<RT, true>(a, cb_r, cb_s, (int)blockIdx.x);
     if (it.group < 0) return;
+    int part = 0;
+    if constexpr (!UP) {                                          // column blocks of a part follow each other
+        const int blocks = pick(it.group >= a.E, cb_s / a.parts_s, cb_r / a.parts_r);
+        part = it.col / blocks;
+        it.col -= part * blocks;
+    }
     MxMatrix m;
     if (!mx_matrix<UP>(a, it.group, &m)) {
         if constexpr (!UP) {                                      // an expert that cannot be used adds nothing
@@ -190,13 +200,14 @@ __global__ __launch_bounds__(256, 2) void mx_tile_kernel(MxArgs a, int cb_r, int
             for (int q = (int)threadIdx.x; q < it.rows * 64; q += 256) {
                 const int r = q >> 6, r0 = it.col * 256 + (q & 63) * 4;
                 if (r0 < sd.cols)
-                    mx_store_y(a.y_fp32, a.y_vec, sd.y, (out0 + r) * sd.ld + r0, sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
+                    mx_store_y(a.y_fp32, a.y_vec, sd.y, part * sd.part + (out0 + r) * sd.ld + r0,
+                               sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
             }
         }
         return;
     }
-    if (m.bits == 4) tile_by_rows<RT, UP, 4>(a, it, m, lds);
-    else tile_by_rows<RT, UP, 8>(a, it, m, lds);
+    if (m.bits == 4) tile_by_rows<RT, UP, 4>(a, it, part, m, lds);
+    else tile_by_rows<RT, UP, 8>(a, it, part, m, lds);
 }
 
 long long mx_max_tiles(const MxArgs& a, int RT);
@@ -204,7 +215,7 @@ long long mx_max_tiles(const MxArgs& a, int RT);
 template <int RT, bool UP>
 static fate_status launch_tile(hipStream_t st, const MxArgs& a) {
     constexpr int width = UP ? 128 : 256;
-    const int cb_r = (a.cols_r + width - 1) / width, cb_s = (a.cols_s + width - 1) / width;
+    const int cb_r = (a.cols_r + width - 1) / width * (UP ? 1 : a.parts_r), cb_s = (a.cols_s + width - 1) / width * (UP ? 1 : a.parts_s);
     const long long items = mx_max_tiles(a, RT) * cb_r + (long long)a.n_shared * ((a.N + RT - 1) / RT) * cb_s;
     const long long grid = (items + 7) / 8 * 8;
     if (grid > 0x7fffffffLL) FATE_FAIL(FATE_ESHAPE, "too many workgroups (%lld)", grid);
@@ -214,17 +225,35 @@ static fate_status launch_tile(hipStream_t st, const MxArgs& a) {
     return FATE_OK;
 }
 
-// rows: of an average group.
-template <bool UP>
-static fate_status launch_by_rows(hipStream_t st, const MxArgs& a, long long rows) {
-    if (rows <= 16) return launch_tile<16, UP>(st, a);
-    if (rows <= 32) return launch_tile<32, UP>(st, a);
-    if (rows <= 64) return launch_tile<64, UP>(st, a);
-    return launch_tile<128, UP>(st, a);
+long long mx_tile_items(const MxArgs& a, bool up, int RT) {
+    const int width = up ? 128 : 256;
+    const long long P = (long long)a.N * a.k, groups = P < a.E ? P : a.E;
+    const long long tiles = groups ? groups * ((P / groups + RT - 1) / RT) : 0;
+    return tiles * ((a.cols_r + width - 1) / width) + (long long)a.n_shared * ((a.N + RT - 1) / RT) * ((a.cols_s + width - 1) / width);
 }
 
-fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up, long long rows) {
-    return up ? launch_by_rows<true>(st, a, rows) : launch_by_rows<false>(st, a, rows);
+// Rows per workgroup.  Groups of experts: half as many again as an average group has, so that most groups are one tile
+// and their weights are read once (64 / 128 rows, us: Mixtral shape 256 tokens 205 / 186, 2048 tokens 770 / 700, Qwen
+// shape with its skewed gate 512 tokens 104 / 123, 1024 tokens 144 / 152).  One dense matrix: as many as leave a
+// workgroup for every compute unit, 128 only where there are several (32 / 64 / 128 rows, us, 4096 x 4096: 512 tokens
+// 17 / 23 / 37, 1024 tokens 28 / 25 / 38, 2048 tokens 52 / 38 / 42).
+int mx_tile_rows(const MxArgs& a, bool up) {
+    if (a.E == 0) {
+        for (int RT = 128; RT > 16; RT /= 2)
+            if (mx_tile_items(a, up, RT) >= (RT == 128 ? 1024 : 256)) return RT;
+        return 16;
+    }
+    const long long P = (long long)a.N * a.k, groups = P < a.E ? P : a.E, rows = P / groups * 3 / 2;
+    return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+}
+
+fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up) {
+    switch (mx_tile_rows(a, up)) {
+        case 16: return up ? launch_tile<16, true>(st, a) : launch_tile<16, false>(st, a);
+        case 32: return up ? launch_tile<32, true>(st, a) : launch_tile<32, false>(st, a);
+        case 64: return up ? launch_tile<64, true>(st, a) : launch_tile<64, false>(st, a);
+        default: return up ? launch_tile<128, true>(st, a) : launch_tile<128, false>(st, a);
+    }
 }
 
 }  // namespace fate

@@ -336,6 +336,13 @@ def test_ffn_mixed_widths_and_sizes(N):
     check_ffn(f, N, 3, N)
 
 
+@pytest.mark.parametrize("N,y_fp32", [(20, True), (40, False), (300, False)])
+def test_ffn_long_reductions_in_parts(N, y_fp32):
+    """A down product of few workgroups and a long reduction is cut into parts; entries shorter than a part's start."""
+    f = Ffn(256, 4, 4608, 4, 1, 4608, 8, sizes=(4608, 32, 2336, 4608), seed=12)
+    check_ffn(f, N, 2, N, y_fp32=y_fp32)
+
+
 @pytest.mark.parametrize("N", [4, 70])
 def test_ffn_absent_and_unreadable_experts(N):
     f = Ffn(256, 6, 256, 4, 1, 128, seed=5, absent=(1, 4))
