@@ -26,8 +26,8 @@ struct NormArgs {
     float eps;
 };
 
-// One row per group of 64 * W threads, W waves (W == 1: four rows per workgroup, no barrier); a thread keeps C pieces
-// of eight elements in registers, so h and delta are read once.
+// One row per 64 * W threads (W == 1: four rows per workgroup, no barrier); a thread keeps C pieces of eight elements in
+// registers, so h and delta are read once.  Memory bounds it: two inputs, up to three outputs.
 template <typename TH, typename TD, int W, int C, bool VEC>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_rmsnorm_kernel(NormArgs a) {
     constexpr int T = 64 * W;
@@ -162,14 +162,12 @@ __global__ __launch_bounds__(256) void mx_pack_weight_kernel(const TS* __restric
 template <typename TH, typename TD, bool VEC>
 static void launch_norm(hipStream_t st, const NormArgs& a) {
     const int pieces = mx_padded(a.H) / 8;
-    // From 2048 rows on there are two waves per SIMD and more without splitting a row, and a row per wave needs no
-    // barrier; with fewer rows a row's latency counts, and it is spread over as many waves as have a piece.
+    // As many waves per row as have a piece of eight elements per thread: rows of a wave each, eight pieces per thread,
+    // need no barrier, but their registers leave fewer loads in flight (16384 rows of 4096 bf16: 143 us; two, four, eight
+    // waves: 119, 111, 105 us, 5.8 TB/s; 512 rows: 14.3 and 10.8).
 #define FATE_NORM(W, C)                                                                                               \
     add_rmsnorm_kernel<TH, TD, W, C, VEC><<<(W) == 1 ? (a.N + 3) / 4 : a.N, (W) == 1 ? 256 : 64 * (W), 0, st>>>(a)
     if (pieces <= 64) FATE_NORM(1, 1);
-    else if (a.N >= 2048 && pieces <= 128) FATE_NORM(1, 2);
-    else if (a.N >= 2048 && pieces <= 256) FATE_NORM(1, 4);
-    else if (a.N >= 2048 && pieces <= 512) FATE_NORM(1, 8);
     else if (pieces <= 128) FATE_NORM(2, 1);
     else if (pieces <= 256) FATE_NORM(4, 1);
     else if (pieces <= 512) FATE_NORM(8, 1);

@@ -243,6 +243,30 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
     const uint8_t* w = a.m.w + (long long)rb * KT * MxWTile<BITS>::kBytes;
     const uint32_t* wsd = reinterpret_cast<const uint32_t*>(a.m.s + (long long)rb * a.m.KG * 256) + lane;
     const int s0 = KT * ks / KS, s1 = KT * (ks + 1) / KS, n = s1 - s0;
+    // rows first (loads return in order), then the weights; the rows are put into LDS while those travel
+    const int per_row = KT * 16, pieces = rows * per_row;         // of eight elements
+    auto fetch = [&](int q) {
+        const int r = q / per_row, i = (q - r * per_row) * 8;
+        const uint16_t* src = a.x + (t0 + r) * a.ld_x + i;
+        v4i v = {0, 0, 0, 0};
+        if (a.x_vec && i + 8 <= a.K) v = ld_global<v4i>(src);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i + e < a.K) v[e >> 1] |= (int)((uint32_t)ld_global<uint16_t>(src, e) << (16 * (e & 1)));
+        }
+        return v;
+    };
+    auto put = [&](int q, v4i v) {
+        const int r = q / per_row, i = (q - r * per_row) * 8;
+        *reinterpret_cast<v4i*>(xl + r * ldx + i) = v;
+    };
+    v4i xv[kStagePieces];
+#pragma unroll
+    for (int i = 0; i < kStagePieces; ++i) {
+        const int q = (int)threadIdx.x + i * kStreamThreads;
+        if (i * kStreamThreads < pieces) xv[i] = fetch(q < pieces ? q : pieces - 1);
+    }
     constexpr int R = 8;
     MxWTile<BITS> wt[R];
     uint32_t sc[R];
@@ -254,22 +278,13 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
             sc[j] = ld_global<uint32_t>(wsd, (s >> 2) * 64);
         }
     }
-    const int per_row = KT * 16, pieces = rows * per_row;         // of eight elements
-    for (int q = (int)threadIdx.x; q < pieces; q += 64 * kStreamWaves) {
-        const int r = q / per_row, i = (q - r * per_row) * 8;
-        const uint16_t* src = a.x + (t0 + r) * a.ld_x + i;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (a.x_vec && i + 8 <= a.K) v = *reinterpret_cast<const uint4*>(src);
-        else {
-            uint32_t d[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (i + e < a.K) d[e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
-            v = make_uint4(d[0], d[1], d[2], d[3]);
-        }
-        *reinterpret_cast<uint4*>(xl + r * ldx + i) = v;
+    for (int i = 0; i < kStagePieces; ++i) {
+        const int q = (int)threadIdx.x + i * kStreamThreads;
+        if (q < pieces) put(q, xv[i]);
     }
-    __syncthreads();
+    for (int q = (int)threadIdx.x + kStagePieces * kStreamThreads; q < pieces; q += kStreamThreads) put(q, fetch(q));
+    lds_only_barrier();
     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
     if (n > 0) {
         const int row = (lane & 15) < rows ? lane & 15 : 0;
