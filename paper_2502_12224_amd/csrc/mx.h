@@ -56,6 +56,9 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax) {
 // 2^(127 - b) for b <= 254 - 2 + 1; a power of two, so multiplying by it rounds nothing that matters.
 __device__ __forceinline__ float mx_inverse_scale(uint32_t b) { return __uint_as_float((254u - (b > 253u ? 253u : b)) << 23); }
 
+// The scale itself (255: infinity, which makes every product with it that is one of codes NaN or infinite).
+__device__ __forceinline__ float mx_scale_f32(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
+
 // Four values over their scale -> four E4M3 codes (the conversion rounds to nearest, ties to even).
 __device__ __forceinline__ uint32_t mx_codes8(float a, float b, float c, float d, uint32_t scale) {
     const float inv = mx_inverse_scale(scale);

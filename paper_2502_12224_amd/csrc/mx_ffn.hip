@@ -5,6 +5,9 @@ namespace fate {
 
 int mx_stream_rows(long long rows, int Kp);
 fate_status launch_mx_stream(hipStream_t st, const MxArgs& a, bool up, int rows_cap);
+bool mx_one_token(const MxArgs& a, size_t* lds);
+fate_status launch_mx_down_one(hipStream_t st, const MxArgs& a, const float* topk_w, const uint8_t* x, const uint8_t* xs,
+                               const uint16_t* gate, void* y, int H, int y_fp32);
 fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up);
 long long mx_tile_items(const MxArgs& a, bool up, int RT);
 int mx_tile_rows(const MxArgs& a, bool up);
@@ -42,7 +45,7 @@ __global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
         for (int i = (int)threadIdx.x * 4; i < a.H; i += threads * 4) {
             const int c = *reinterpret_cast<const int*>(a.x + t * a.Kp + i);
             const uint32_t b = a.xs[(t * a.Kp + i) / kMxBlock];
-            const float f = b == 255u ? __builtin_nanf("") : __uint_as_float(b ? b << 23 : 0x400000u);
+            const float f = mx_scale_f32(b);
             const uint2 w = *reinterpret_cast<const uint2*>(a.gate + i);
             dot += f * (__builtin_amdgcn_cvt_f32_fp8(c, 0) * bf16_lo(w.x) + __builtin_amdgcn_cvt_f32_fp8(c, 1) * bf16_hi(w.x) +
                         __builtin_amdgcn_cvt_f32_fp8(c, 2) * bf16_lo(w.y) + __builtin_amdgcn_cvt_f32_fp8(c, 3) * bf16_hi(w.y));
@@ -246,6 +249,11 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     a.parts_r = a.parts_s = 1;
     a.part_r = (long long)d->N * d->k * d->H;
     a.part_s = (long long)d->N * d->n_shared * d->H;
+    const uint16_t* gate = d->n_shared ? static_cast<const uint16_t*>(shared_gate_bf16) : nullptr;
+    size_t lds;
+    if (mx_one_token(a, &lds))
+        return launch_mx_down_one(st, a, topk_w, static_cast<const uint8_t*>(x_codes), static_cast<const uint8_t*>(x_scales),
+                                  gate, y, d->H, d->y_is_fp32);
     const bool streamed = stream_rows(a, false) != 0;
     a.y_fp32 = d->y_is_fp32 || streamed;                          // (few rows: their bytes do not count)
     if (!streamed) {
@@ -261,7 +269,7 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     if (s != FATE_OK) return s;
 
     MxCombineArgs c{base + w.rows_r, base + w.rows_s, inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
-                    static_cast<const uint8_t*>(x_scales), d->n_shared ? static_cast<const uint16_t*>(shared_gate_bf16) : nullptr,
+                    static_cast<const uint8_t*>(x_scales), gate,
                     y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H), a.parts_r, a.parts_s, a.part_r, a.part_s};
     const int threads = d->H >= 4096 ? 1024 : (d->H + 255) / 256 * 64;
     if (d->y_is_fp32) mx_combine_kernel<float, float><<<d->N, threads, 0, st>>>(c);

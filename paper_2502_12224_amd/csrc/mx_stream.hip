@@ -187,12 +187,174 @@ __global__ __launch_bounds__(kStreamThreads, 4) void mx_stream_kernel(MxArgs a, 
     }
 }
 
+// ---- one token: the down products of all its experts and their sum -------------------------------------------------
+
+// A workgroup owns 16 outputs.  The tiles of all terms (the token's experts in sorted order, then the shared ones) form one
+// list of steps of 128 columns, of which each of the 16 waves takes an equal share, whoever's they are; a wave weighs a
+// term's sum when the term ends, and the waves' sums meet in LDS.  So there are no rows to write and to add up again, and
+// no third launch (one token, Qwen shape: 11.7 us for the two kernels, 9.5 for this one).  Lane t of every wave knows term t.
+constexpr int kOneWaves = 16, kOneRing = 6;
+
+struct MxOneArgs {
+    MxArgs a;                           // the down product's arguments, y_s / y_r unused
+    const float* topk_w;
+    const uint8_t* x; const uint8_t* xs; const uint16_t* gate;
+    void* y;
+    int H, y_fp32;
+};
+
+__global__ __launch_bounds__(64 * kOneWaves) void mx_down_one_kernel(MxOneArgs o) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ float gsum[kOneWaves];
+    const MxArgs& a = o.a;
+    v4f* red = reinterpret_cast<v4f*>(lds);                       // [16 waves][4]
+    uint8_t* hr = lds + kOneWaves * 64;                           // [k][Kp_r], [n_shared][Kp_s], then the scales
+    uint8_t* hs = hr + a.k * a.Kp_r;
+    uint8_t* sr = hs + a.n_shared * a.Kp_s;
+    uint8_t* ss = sr + a.k * a.Kp_r / 32;
+    const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = uni((int)(threadIdx.x >> 6));
+    const int terms = a.k + a.n_shared;
+
+    // Requests in the order in which they are waited for: where the experts' rows end, which weight a position has, the
+    // rows of h (contiguous) and what the shared gate needs; then the entries, then weights.
+    int ends[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = lane * 4 + i;
+        ends[i] = e < a.E ? ld_global<int>(a.offsets, e + 1) : 0x7fffffff;
+    }
+    const int pair = ld_global<int>(a.perm, lane < a.k ? lane : 0);
+    const int n0 = a.k * (a.Kp_r / 16), n1 = n0 + a.n_shared * (a.Kp_s / 16);
+    auto piece = [&](int q, uint32_t* c) {
+        const bool r = q < n0;
+        const int i = r ? q : q - n0;
+        *c = ld_global<uint32_t>(pick(r, a.xs_r, a.xs_s), i >> 3);
+        return ld_global<v4i>(pick(r, a.x_r, a.x_s), i);
+    };
+    auto put = [&](int q, v4i v, uint32_t c) {
+        const bool r = q < n0;
+        const int i = r ? q : q - n0;
+        *reinterpret_cast<v4i*>((r ? hr : hs) + i * 16) = v;
+        if ((i & 7) == 0) *reinterpret_cast<uint32_t*>((r ? sr : ss) + (i >> 3) * 4) = c;
+    };
+    uint32_t hc;
+    const v4i hv = piece((int)threadIdx.x < n1 ? (int)threadIdx.x : n1 - 1, &hc);
+    auto dot4 = [&](int i) {                                      // four columns of x . gate
+        const int c = ld_global<int>(o.x + i);
+        const long long w = ld_global<long long>(o.gate + i);
+        const uint32_t w0 = (uint32_t)w, w1 = (uint32_t)((unsigned long long)w >> 32);
+        return mx_scale_f32(ld_global<uint8_t>(o.xs, i / kMxBlock)) *
+               (__builtin_amdgcn_cvt_f32_fp8(c, 0) * bf16_lo(w0) + __builtin_amdgcn_cvt_f32_fp8(c, 1) * bf16_hi(w0) +
+                __builtin_amdgcn_cvt_f32_fp8(c, 2) * bf16_lo(w1) + __builtin_amdgcn_cvt_f32_fp8(c, 3) * bf16_hi(w1));
+    };
+    float dot = 0.0f;
+    if (o.gate != nullptr)
+        for (int i = (int)threadIdx.x * 4; i < o.H; i += 256 * kOneWaves) dot += dot4(i);
+
+    int expert = a.E;
+    for (int t = 0; t < a.k; ++t) {
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) before += __builtin_popcountll(__ballot(ends[i] <= t));
+        expert = lane == t ? before : expert;
+    }
+    const bool shared = lane >= a.k;
+    const bool exists = lane < terms && (shared || expert < a.E);
+    const fate_qexpert* p = shared ? a.shared + (lane - a.k) : a.experts + expert;
+    v4i q0 = {0, 0, 0, 0}, q1 = q0, q2 = q0, q3 = q0, q4 = q0;
+    float weight = 1.0f;
+    if (exists) {
+        q0 = ld_global<v4i>(p, 0); q1 = ld_global<v4i>(p, 1); q2 = ld_global<v4i>(p, 2); q3 = ld_global<v4i>(p, 3);
+        q4 = ld_global<v4i>(p, 4);
+        if (!shared) weight = ld_global<float>(o.topk_w, pair);
+    }
+    const int bits = q3[0], I = q3[2];
+    const bool absent = exists && q0[0] == 0 && q0[1] == 0;
+    const bool unread = exists && !absent &&
+                        ((bits != 4 && bits != 8) || q3[1] != kMxBlock || I < kMxBlock || I % kMxBlock ||
+                         I > (shared ? a.K_s : a.K_r) || q4[0] != 0 || q4[1] != 0);
+    if (blockIdx.x == 0 && wave == 0 && (absent || unread)) atomicOr(a.status, absent ? 1 : 4);
+    const int KT = exists && !absent && !unread ? mx_steps(I) : 0;
+    const int incl = wave_scan_inclusive(KT);
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    const int first = total * wave / kOneWaves, last = total * (wave + 1) / kOneWaves;
+
+    // step q of the list: its term, the tile and the scales of it
+    MxWTile<8> wt[kOneRing];
+    uint32_t sc[kOneRing];
+    auto term_of = [&](int q) { return (int)__builtin_ctzll(__ballot(incl > q)); };
+    auto load = [&](int j, int q) {
+        const int t = term_of(q);
+        auto scalar = [&](int v) { return (unsigned long long)(uint32_t)__builtin_amdgcn_readlane(v, t); };
+        const int steps = (int)scalar(KT), s = q - ((int)scalar(incl) - steps), b = (int)scalar(bits);
+        const uint8_t* w = reinterpret_cast<const uint8_t*>(scalar(q1[1]) << 32 | scalar(q1[0]));
+        const uint8_t* ws = reinterpret_cast<const uint8_t*>(scalar(q2[3]) << 32 | scalar(q2[2]));
+        const long long tile = (long long)blockIdx.x * steps + s;
+        const uint8_t* wp = w + tile * (b == 4 ? 1024 : 2048);
+        const v4i lo = ld_global<v4i>(wp, lane), hi = ld_global<v4i>(wp, b == 4 ? lane : 64 + lane);
+        wt[j].v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        sc[j] = ld_global<uint32_t>(ws, ((long long)blockIdx.x * ((steps + 3) / 4) + (s >> 2)) * 64 + lane);
+    };
+    if (first < last) {
+#pragma unroll
+        for (int j = 0; j < kOneRing; ++j) load(j, first + j < last ? first + j : last - 1);
+    }
+    if ((int)threadIdx.x < n1) put((int)threadIdx.x, hv, hc);
+    for (int q = (int)threadIdx.x + 64 * kOneWaves; q < n1; q += 64 * kOneWaves) {
+        const v4i v = piece(q, &hc);
+        put(q, v, hc);
+    }
+    dot = wave_sum(dot);
+    if (lane == 0) gsum[wave] = dot;
+    lds_only_barrier();                                           // h is in LDS
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f}, shared_sum = sum, acc = sum;
+    for (int base = first; base < last; base += kOneRing) {
+        const bool more = base + kOneRing < last;
+#pragma unroll
+        for (int j = 0; j < kOneRing; ++j) {
+            const int q = base + j;
+            if (q < last) {
+                const int t = term_of(q), end = __builtin_amdgcn_readlane(incl, t);
+                const int s = q - (end - __builtin_amdgcn_readlane(KT, t));
+                // (all 16 columns of the product are the one row)
+                const uint8_t* xr = t < a.k ? hr + t * a.Kp_r : hs + (t - a.k) * a.Kp_s;
+                const uint8_t* xc = t < a.k ? sr + t * (a.Kp_r / 32) : ss + (t - a.k) * (a.Kp_s / 32);
+                const v4i lo = *reinterpret_cast<const v4i*>(xr + s * kMxStep + 16 * g);
+                const v4i hi = *reinterpret_cast<const v4i*>(xr + s * kMxStep + 64 + 16 * g);
+                const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                const uint32_t ws = sc[j] >> (8 * (s & 3)), xs = xc[s * 4 + g];
+                if (__builtin_amdgcn_readlane(bits, t) == 4)
+                    acc = mx_mfma4<0>(__builtin_shufflevector(wt[j].v, wt[j].v, 0, 1, 2, 3), ws, x, xs, acc);
+                else acc = wt[j].mfma<0>(ws, x, xs, acc);
+                if (q + 1 == end || q + 1 == last) {
+                    if (t < a.k) sum += read_lane_f32(weight, t) * acc;
+                    else shared_sum += acc;
+                    acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+            }
+            if (more) load(j, q + kOneRing < last ? q + kOneRing : last - 1);
+        }
+    }
+    float gate = 1.0f;
+    if (o.gate != nullptr) {
+        dot = 0.0f;
+        for (int w = 0; w < kOneWaves; ++w) dot += gsum[w];
+        gate = 1.0f / (1.0f + __expf(-dot));
+    }
+    if ((lane & 15) == 0) red[wave * 4 + g] = sum + gate * shared_sum;
+    __syncthreads();
+    if (threadIdx.x < 4) {
+        v4f y = red[threadIdx.x];
+        for (int w = 1; w < kOneWaves; ++w) y += red[w * 4 + threadIdx.x];
+        const int r0 = (int)blockIdx.x * 16 + 4 * (int)threadIdx.x;
+        mx_store_y(o.y_fp32, true, o.y, r0, o.H - r0, y);
+    }
+}
+
 // ---- bf16 rows: weights become the bf16 numbers they are ----------------------------------------------------------
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ float mx_scale_f32(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
 
 template <int SEL4>
 __device__ __forceinline__ v2bf mx_pair4(uint32_t d, float s) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, s, SEL4); }
@@ -392,6 +554,21 @@ fate_status launch_mx_stream(hipStream_t st, const MxArgs& a, bool up, int rows_
         case 4: return go(mx_stream_kernel<false, 4>, 32);
         default: return go(mx_stream_kernel<false, 8>, 16);
     }
+}
+
+// One token's down products and their sum; false: too many terms, or their rows do not fit into LDS.
+bool mx_one_token(const MxArgs& a, size_t* lds) {
+    *lds = kOneWaves * 64 + (size_t)(a.k * (long long)a.Kp_r + a.n_shared * (long long)a.Kp_s) / 32 * 33;
+    return a.N == 1 && a.k + a.n_shared <= 64 && *lds <= 64 * 1024;
+}
+
+fate_status launch_mx_down_one(hipStream_t st, const MxArgs& a, const float* topk_w, const uint8_t* x, const uint8_t* xs,
+                               const uint16_t* gate, void* y, int H, int y_fp32) {
+    size_t lds = 0;
+    mx_one_token(a, &lds);
+    mx_down_one_kernel<<<(unsigned)(H / 16), 64 * kOneWaves, lds, st>>>(MxOneArgs{a, topk_w, x, xs, gate, y, H, y_fp32});
+    FATE_HIP(hipGetLastError());
+    return FATE_OK;
 }
 
 fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x, const MxMatrix& m, const float* bias,

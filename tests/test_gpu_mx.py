@@ -336,6 +336,22 @@ def test_ffn_mixed_widths_and_sizes(N):
     check_ffn(f, N, 3, N)
 
 
+@pytest.mark.parametrize("E,k,ns,gate,y_fp32", [(1, 1, 0, False, True), (200, 8, 2, True, True), (256, 20, 3, True, False),
+                                                (7, 3, 1, False, False), (70, 64, 1, True, True)])
+def test_ffn_single_token(E, k, ns, gate, y_fp32):
+    """One token: all its down products in one launch, many terms, experts named twice, absent ones, other widths."""
+    f = Ffn(96, E, 64 if E > 100 else 288, (4, 8), ns, 480, 8, sizes=(64, 32) if E > 100 else (288, 96, 32), seed=E + k,
+            absent=(E - 1,) if E > 1 else ())
+    r, _ = routing(1, k, E, 5)
+    status = 1 if E > 1 and E - 1 in r else 0
+    check_ffn(f, 1, k, 4, y_fp32=y_fp32, gate=gate and ns > 0, status=status)
+    ids = r.clone()
+    ids[0, k // 2:] = ids[0, 0]
+    if E > 1:
+        ids[0, k - 1] = E - 1
+    check_ffn(f, 1, k, 4, y_fp32=y_fp32, gate=gate and ns > 0, ids=ids, status=1 if E > 1 else 0)
+
+
 @pytest.mark.parametrize("N,y_fp32", [(20, True), (40, False), (300, False)])
 def test_ffn_long_reductions_in_parts(N, y_fp32):
     """A down product of few workgroups and a long reduction is cut into parts; entries shorter than a part's start."""
