@@ -150,7 +150,8 @@ typedef struct {
     const void* s3;
     const void* s2; /* fp16 scales, group-major [I/group, H] */
     int32_t bits;   /* 2, 4 or 8: width of THIS copy */
-    int32_t group;  /* multiple of 64 */
+    int32_t group;  /* multiple of 64; 32: block-scaled matrices of fate_mx_pack_weight, which fate_moe_ffn_mx reads and
+                       the other calls do not */
     int32_t I;      /* intermediate size, multiple of 64 */
     int32_t reserved;
     /* fp16 zero-points per group, laid out like the scales (group-major), or NULL for the symmetric
@@ -388,7 +389,7 @@ fate_status fate_add_rmsnorm(void* stream, int N, int H, const void* h, int h_ty
  * of y_type FATE_BF16 or FATE_FP32, rows ld_y elements apart.
  * x_type FATE_BF16: x [N,K], rows ld_x apart, x_scales NULL; the weights enter as
  *   the bf16 numbers that they are, for few tokens (all N are right, weights are
- *   read once per 16 tokens).
+ *   read once per 16 tokens); K <= 65536.
  * x_type FATE_MXFP8: 8-bit rows x, x_scales (ld_x is not read), at twice the
  *   matrix rate.  The 8-bit matrix instruction adds up eight products at a time
  *   with 16 bits below the largest of them: y is within 2.2e-4 of the sum of
@@ -412,9 +413,9 @@ fate_status fate_mx_linear(void* stream, int N, int K, int R, const void* x, int
  * (the widths of a layer may be mixed), group 32, I a multiple of 32 up to
  * I_max, no zero-points; so the expert cache and its copy engine move them like
  * any others.  Descriptor: group and shared_group 32, H, I_max and I_shared_max
- * multiples of 32, mode 0.  An activated expert whose w1 is NULL is flagged in
- * the int32 at workspace offset 0 (bit 0) and contributes nothing, as does (bit 2)
- * an entry of another format.  Sums as in fate_mx_linear; the rows of the down
+ * multiples of 32, mode 0.  An activated expert with a NULL matrix or scale is
+ * flagged in the int32 at workspace offset 0 (bit 0; the caller clears it) and
+ * contributes nothing, as does (bit 2) an entry of another format.  Sums as in fate_mx_linear; the rows of the down
  * product (of long reductions: of parts of it) are kept in fp32, or, for more than
  * a few tokens, in y's type until they are added up in fp32.
  * workspace: what calls of up to N tokens need; calls that share one are ordered

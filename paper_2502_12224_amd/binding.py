@@ -513,6 +513,15 @@ def fate_moe_ffn_mx(desc, x_codes, x_scales, experts_dev, counts, offsets, perm,
     N, H = desc.N, desc.H
     _check_mx(x_codes, x_scales, N, H)
     _dense(y, "y", torch.float32 if desc.y_is_fp32 else torch.bfloat16, (N, H))
+    P, E, i32 = N * desc.k, desc.E, torch.int32
+    if counts.dtype != i32 or offsets.dtype != i32 or perm.dtype != i32 or inv_perm.dtype != i32 or \
+            expert_order.dtype != i32 or topk_w.dtype != torch.float32:
+        _refuse("counts, offsets, perm, inv_perm and expert_order are int32, topk_w is fp32")
+    if offsets.numel() <= E or perm.numel() < P or inv_perm.numel() < P or topk_w.numel() < P or \
+            experts_dev.nbytes < E * 96 or (desc.n_shared and (shared_dev is None or shared_dev.nbytes < desc.n_shared * 96)):
+        _refuse("a routing output or an expert table is smaller than the descriptor says")
+    if shared_gate is not None and (shared_gate.dtype != torch.bfloat16 or shared_gate.numel() < H):
+        _refuse("shared_gate is a bf16 vector [H]")
     _check(lib().fate_moe_ffn_mx(_here(stream, x_codes, x_scales, experts_dev, counts, offsets, perm, inv_perm,
                                        expert_order, topk_w, shared_dev, shared_gate, y, workspace), C.addressof(desc),
                                  x_codes.data_ptr(), x_scales.data_ptr(), _ptr(experts_dev), _ptr(counts), _ptr(offsets),

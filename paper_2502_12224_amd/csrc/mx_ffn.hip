@@ -161,6 +161,7 @@ extern "C" fate_status fate_mx_linear(void* stream, int N, int K, int R, const v
                                       const void* x_scales, int bits, const void* w_codes, const void* w_scales,
                                       const float* bias, void* y, int y_type, int64_t ld_y) {
     if (N < 0) FATE_FAIL(FATE_EINVAL, "N = %d < 0", N);
+    if (N > (1 << 30)) FATE_FAIL(FATE_ESHAPE, "N = %d > 2^30", N);
     if (K < 1 || K > (1 << 24) || R < 1 || R > (1 << 24))
         FATE_FAIL(FATE_ESHAPE, "K = %d, R = %d (1 to 2^24 each)", K, R);
     if (bits != 4 && bits != 8) FATE_FAIL(FATE_EINVAL, "bits = %d (4 or 8)", bits);
@@ -212,6 +213,8 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     FATE_CHECK_PTR(x_scales);
     FATE_CHECK_PTR(y);
     FATE_CHECK_PTR_OPT(shared_gate_bf16);
+    FATE_CHECK_PTR_OPT(experts_dev);
+    FATE_CHECK_PTR_OPT(shared_dev);
     if (!experts_dev || !counts || !offsets || !perm || !inv_perm || !expert_order || !topk_w)
         FATE_FAIL(FATE_EINVAL, "experts, counts, offsets, perm, inv_perm, expert_order and topk_w must not be NULL");
     if (d->n_shared && !shared_dev) FATE_FAIL(FATE_EINVAL, "shared_dev is NULL with n_shared = %d", d->n_shared);

@@ -165,10 +165,15 @@ __device__ __forceinline__ bool mx_matrix(const MxArgs& a, int group, MxMatrix* 
         return reinterpret_cast<const uint8_t*>(((unsigned long long)(uint32_t)uni(hi) << 32) | (uint32_t)uni(lo));
     };
     const uint8_t* w1 = pointer(q0[0], q0[1]);
+    const uint8_t* w3 = pointer(q0[2], q0[3]);
+    const uint8_t* w2 = pointer(q1[0], q1[1]);
+    const uint8_t* s1 = pointer(q1[2], q1[3]);
+    const uint8_t* s3 = pointer(q2[0], q2[1]);
+    const uint8_t* s2 = pointer(q2[2], q2[3]);
     const int bits = uni(q3[0]), group_size = uni(q3[1]), I = uni(q3[2]);
     const int I_max = pick(a.down != 0, pick(shared, a.K_s, a.K_r), pick(shared, a.cols_s, a.cols_r));
     int bit = 0;
-    if (w1 == nullptr) bit = 1;
+    if (!w1 || !w3 || !w2 || !s1 || !s3 || !s2) bit = 1;
     else if ((bits != 4 && bits != 8) || group_size != kMxBlock || I < kMxBlock || I % kMxBlock || I > I_max ||
              pointer(q4[0], q4[1]) != nullptr) bit = 4;
     if (bit) {
@@ -176,10 +181,10 @@ __device__ __forceinline__ bool mx_matrix(const MxArgs& a, int group, MxMatrix* 
         return false;
     }
     const int K = pick(a.down != 0, I, pick(shared, a.K_s, a.K_r));
-    m->w = UP ? w1 : pointer(q1[0], q1[1]);
-    m->s = UP ? pointer(q1[2], q1[3]) : pointer(q2[2], q2[3]);
-    m->w3 = pointer(q0[2], q0[3]);
-    m->s3 = pointer(q2[0], q2[1]);
+    m->w = UP ? w1 : w2;
+    m->s = UP ? s1 : s2;
+    m->w3 = w3;
+    m->s3 = s3;
     m->bits = bits;
     m->KT = mx_steps(K);
     m->KG = mx_step_groups(K);

@@ -32,7 +32,7 @@ template <typename TH, typename TD, int W, int C, bool VEC>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_rmsnorm_kernel(NormArgs a) {
     constexpr int T = 64 * W;
     __shared__ float part[W];
-    const int row = W == 1 ? (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6) : (int)blockIdx.x;
+    const long long row = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : (long long)blockIdx.x;
     const int t = W == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
     if (row >= a.N) return;                              // whole waves (W == 1); never otherwise
     const TH* h = static_cast<const TH*>(a.h) + row * a.ld_h;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_rmsnorm_kernel(Norm
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = j < n ? x[j] : 0.0f;
             }
-            quantize8(x, a.codes + (long long)row * Hp + i, a.scales + ((long long)row * Hp + i) / kMxBlock);
+            quantize8(x, a.codes + row * Hp + i, a.scales + (row * Hp + i) / kMxBlock);
         }
     }
 }
@@ -166,7 +166,7 @@ static void launch_norm(hipStream_t st, const NormArgs& a) {
     // need no barrier, but their registers leave fewer loads in flight (16384 rows of 4096 bf16: 143 us; two, four, eight
     // waves: 119, 111, 105 us, 5.8 TB/s; 512 rows: 14.3 and 10.8).
 #define FATE_NORM(W, C)                                                                                               \
-    add_rmsnorm_kernel<TH, TD, W, C, VEC><<<(W) == 1 ? (a.N + 3) / 4 : a.N, (W) == 1 ? 256 : 64 * (W), 0, st>>>(a)
+    add_rmsnorm_kernel<TH, TD, W, C, VEC><<<(W) == 1 ? (a.N - 1) / 4 + 1 : a.N, (W) == 1 ? 256 : 64 * (W), 0, st>>>(a)
     if (pieces <= 64) FATE_NORM(1, 1);
     else if (pieces <= 128) FATE_NORM(2, 1);
     else if (pieces <= 256) FATE_NORM(4, 1);

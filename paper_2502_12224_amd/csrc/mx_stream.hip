@@ -269,7 +269,8 @@ __global__ __launch_bounds__(64 * kOneWaves) void mx_down_one_kernel(MxOneArgs o
         if (!shared) weight = ld_global<float>(o.topk_w, pair);
     }
     const int bits = q3[0], I = q3[2];
-    const bool absent = exists && q0[0] == 0 && q0[1] == 0;
+    auto null = [](const v4i& q, int i) { return q[i] == 0 && q[i + 1] == 0; };
+    const bool absent = exists && (null(q0, 0) || null(q0, 2) || null(q1, 0) || null(q1, 2) || null(q2, 0) || null(q2, 2));
     const bool unread = exists && !absent &&
                         ((bits != 4 && bits != 8) || q3[1] != kMxBlock || I < kMxBlock || I % kMxBlock ||
                          I > (shared ? a.K_s : a.K_r) || q4[0] != 0 || q4[1] != 0);

@@ -52,6 +52,7 @@ def test_linear_refusals():
 
     def call(**kw):
         return f(0, *{**good, **kw}.values())
+    assert call(N=(1 << 30) + 1, xt=2, xs=P) == ESHAPE
     assert call(N=-1) == EINVAL and call(K=0) == ESHAPE and call(R=0) == ESHAPE and call(bits=2) == EINVAL
     assert call(xt=1) == EINVAL and call(yt=2) == EINVAL and call(ldx=255) == ESHAPE and call(ldy=99) == ESHAPE
     assert call(xs=P) == EINVAL and call(K=65537, ldx=65537) == ESHAPE
@@ -87,6 +88,7 @@ def test_ffn_refusals():
     assert call(1, None) == EINVAL and call(2, 0) == EINVAL and call(3, ODD) == EALIGN
     for i in (4, 5, 6, 7, 8, 9, 10):
         assert call(i, 0) == EINVAL, i
+    assert call(4, ODD) == EALIGN and call(11, ODD) == EALIGN
     assert call(11, 0) == EINVAL and call(12, ODD) == EALIGN and call(13, 0) == EINVAL
     assert call(14, 0) == EWORKSPACE and call(15, need - 1) == EWORKSPACE and call(14, ODD) == EALIGN
     d0 = _desc(N=0)

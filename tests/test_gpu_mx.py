@@ -336,6 +336,21 @@ def test_ffn_mixed_widths_and_sizes(N):
     check_ffn(f, N, 3, N)
 
 
+def test_ffn_binding_refusals():
+    f = Ffn(64, 4, 64, 4, 1, 64, seed=1)
+    ids, w = routing(3, 2, 4, 1)
+    d, tabs, mx = f.desc(3, 2), gpu_permute(ids.to(DEV), 4), B.mx_empty(3, 64)
+    B.fate_mx_quantize(torch.zeros(3, 64, device=DEV), *mx)
+    ws = torch.zeros(B.fate_moe_ffn_mx_workspace(d), dtype=torch.uint8, device=DEV)
+    good = [d, *mx, f.table, *tabs, w.to(DEV), f.shared_table, None, torch.empty(3, 64, device=DEV), ws]
+    B.fate_moe_ffn_mx(*good)
+    for i, bad in [(1, mx[0][:2]), (2, mx[1].cpu()), (3, f.table[:100]), (4, tabs[0].long()), (5, tabs[1][:4]), (6, tabs[2].long()),
+                   (7, tabs[3][:5]), (9, w.to(DEV).double()), (9, w.to(DEV)[:2]), (10, None), (10, f.shared_table[:50]),
+                   (11, torch.zeros(64, device=DEV)), (12, torch.empty(3, 64, device=DEV, dtype=torch.bfloat16)), (13, ws[:-300])]:
+        with pytest.raises(B.FateError):
+            B.fate_moe_ffn_mx(*good[:i], bad, *good[i + 1:])
+
+
 @pytest.mark.parametrize("E,k,ns,gate,y_fp32", [(1, 1, 0, False, True), (200, 8, 2, True, True), (256, 20, 3, True, False),
                                                 (7, 3, 1, False, False), (70, 64, 1, True, True)])
 def test_ffn_single_token(E, k, ns, gate, y_fp32):
@@ -368,6 +383,12 @@ def test_ffn_absent_and_unreadable_experts(N):
     f.table = B.expert_table(f.structs)
     del f.numbers[2]
     check_ffn(f, N, 3, N, status=5)
+    if N > 4:                                   # a table entry that is only partly there
+        f.structs[0].w2 = None
+        f.structs[3].s3 = None
+        f.table = B.expert_table(f.structs)
+        del f.numbers[0], f.numbers[3]
+        check_ffn(f, N, 3, N, status=5)
     f.structs = [B.fate_qexpert(0, 0, 0, 0, 0, 0, 4, 32, 256, 0)] * 6
     f.table, f.numbers, f.shared_table, f.n_shared, f.shared = B.expert_table(f.structs), {}, None, 0, []
     y = check_ffn(f, N, 3, N, status=1)
