@@ -24,55 +24,56 @@ struct MxCombineArgs {
     long long part_r, part_s;
 };
 
+// Eight consecutive columns of a row, times w, onto y.
 template <typename T>
-__device__ __forceinline__ v4f row4(const void* rows, long long at) {
-    if constexpr (sizeof(T) == 4) return reinterpret_cast<const v4f*>(static_cast<const float*>(rows) + at)[0];
-    else {
-        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(rows) + at);
-        return v4f{bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y)};
-    }
+__device__ __forceinline__ void add_row8(const void* rows, long long at, float w, float (&y)[8]) {
+    float v[8];
+    load8<true>(static_cast<const T*>(rows) + at, 8, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fmaf(w, v[i], y[i]);
 }
 
 // y[t] = sum_j w[t,j] row[inv_perm[t,j]] + g(t) sum_v shared row: one workgroup per token, terms in the order of j, then v.
-// The rows are requested before the gate is known; what is left is two round trips and the launch.
+// Few tokens: two round trips and the launch (the rows are requested before the gate is known); many: memory.
 template <typename T, typename TY>
-__global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
-    __shared__ float part[16];
+__global__ __launch_bounds__(512) void mx_combine_kernel(MxCombineArgs a) {
+    __shared__ float part[8];
     const long long t = blockIdx.x;
     const int P = a.N * a.k, threads = (int)blockDim.x;
     float dot = 0.0f;
     if (a.gate != nullptr) {
         for (int i = (int)threadIdx.x * 4; i < a.H; i += threads * 4) {
             const int c = *reinterpret_cast<const int*>(a.x + t * a.Kp + i);
-            const uint32_t b = a.xs[(t * a.Kp + i) / kMxBlock];
-            const float f = mx_scale_f32(b);
+            const float f = mx_scale_f32(a.xs[(t * a.Kp + i) / kMxBlock]);
             const uint2 w = *reinterpret_cast<const uint2*>(a.gate + i);
             dot += f * (__builtin_amdgcn_cvt_f32_fp8(c, 0) * bf16_lo(w.x) + __builtin_amdgcn_cvt_f32_fp8(c, 1) * bf16_hi(w.x) +
                         __builtin_amdgcn_cvt_f32_fp8(c, 2) * bf16_lo(w.y) + __builtin_amdgcn_cvt_f32_fp8(c, 3) * bf16_hi(w.y));
         }
     }
     float gate = 1.0f;
-    for (int i0 = 0; i0 < a.H; i0 += threads * 4) {
-        const int i = i0 + (int)threadIdx.x * 4;
-        v4f y = {0.0f, 0.0f, 0.0f, 0.0f}, z = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (i < a.H) {
-            for (int j0 = 0; j0 < a.k; j0 += 8) {
-                int s[8];
-                float w[8];
+    for (int i0 = 0; i0 < a.H; i0 += threads * 8) {
+        const int i = i0 + (int)threadIdx.x * 8;
+        float y[8], z[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+        for (int c = 0; c < 8; ++c) y[c] = z[c] = 0.0f;
+        if (i < a.H) {
+            for (int j0 = 0; j0 < a.k; j0 += 4) {
+                int s[4];
+                float w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
                     const int at = j0 + j < a.k ? j0 + j : a.k - 1;
                     s[j] = a.inv_perm[t * a.k + at];
                     w[j] = a.topk_w[t * a.k + at];
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < 4; ++j)
                     if (j0 + j < a.k && (unsigned)s[j] < (unsigned)P)
-                        for (int p = 0; p < a.parts_r; ++p) y += w[j] * row4<T>(a.rows_r, p * a.part_r + (long long)s[j] * a.H + i);
+                        for (int p = 0; p < a.parts_r; ++p) add_row8<T>(a.rows_r, p * a.part_r + (long long)s[j] * a.H + i, w[j], y);
             }
             for (int v = 0; v < a.n_shared * a.parts_s; ++v) {
                 const int p = v / a.n_shared;
-                z += row4<T>(a.rows_s, p * a.part_s + ((long long)(v - p * a.n_shared) * a.N + t) * a.H + i);
+                add_row8<T>(a.rows_s, p * a.part_s + ((long long)(v - p * a.n_shared) * a.N + t) * a.H + i, 1.0f, z);
             }
         }
         if (a.gate != nullptr && i0 == 0) {
@@ -83,11 +84,10 @@ __global__ __launch_bounds__(1024) void mx_combine_kernel(MxCombineArgs a) {
             for (int p = 0; p < threads / 64; ++p) dot += part[p];
             gate = 1.0f / (1.0f + __expf(-dot));
         }
-        y += gate * z;
         if (i < a.H) {
-            if constexpr (sizeof(TY) == 4) *reinterpret_cast<v4f*>(static_cast<float*>(a.y) + t * a.H + i) = y;
-            else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + t * a.H + i) =
-                     make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+#pragma unroll
+            for (int c = 0; c < 8; ++c) y[c] = fmaf(gate, z[c], y[c]);
+            store8<true>(static_cast<TY*>(a.y) + t * a.H + i, 8, y);
         }
     }
 }
@@ -274,7 +274,7 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     MxCombineArgs c{base + w.rows_r, base + w.rows_s, inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
                     static_cast<const uint8_t*>(x_scales), gate,
                     y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H), a.parts_r, a.parts_s, a.part_r, a.part_s};
-    const int threads = d->H >= 4096 ? 1024 : (d->H + 255) / 256 * 64;
+    const int threads = d->H >= 4096 ? 512 : (d->H + 511) / 512 * 64;
     if (d->y_is_fp32) mx_combine_kernel<float, float><<<d->N, threads, 0, st>>>(c);
     else if (a.y_fp32) mx_combine_kernel<float, uint16_t><<<d->N, threads, 0, st>>>(c);
     else mx_combine_kernel<uint16_t, uint16_t><<<d->N, threads, 0, st>>>(c);
