@@ -81,13 +81,20 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
     return v > o ? v : o;
 }
 
+// Sixteen bytes wherever an element may start: global accesses need no alignment, the compiler only has to be told.
+typedef v4i v4i_at2 __attribute__((aligned(2)));
+typedef v4i v4i_at4 __attribute__((aligned(4)));
+
 // Eight consecutive elements, of which the first `n` exist.  VEC: all eight exist and lie on a 16-byte boundary.
 template <bool VEC>
 __device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
-    if constexpr (VEC) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p);
-        v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
-        v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
+    if (VEC || n >= 8) {
+        const v4i q = VEC ? *reinterpret_cast<const v4i*>(p) : *reinterpret_cast<const v4i_at2*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = bf16_lo((uint32_t)q[i]);
+            v[2 * i + 1] = bf16_hi((uint32_t)q[i]);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_bits_to_f32(p[i]) : 0.0f;
@@ -95,9 +102,14 @@ __device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
 }
 template <bool VEC>
 __device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
-    if constexpr (VEC) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    if (VEC || n >= 8) {
+        const v4i a = VEC ? reinterpret_cast<const v4i*>(p)[0] : reinterpret_cast<const v4i_at4*>(p)[0];
+        const v4i b = VEC ? reinterpret_cast<const v4i*>(p)[1] : reinterpret_cast<const v4i_at4*>(p)[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = __int_as_float(a[i]);
+            v[4 + i] = __int_as_float(b[i]);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
@@ -108,9 +120,10 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }
 template <bool VEC>
 __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
-    if constexpr (VEC) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]),
-                                                  bf16_pair(v[6], v[7]));
+    if (VEC || n >= 8) {
+        const v4i q = {(int)bf16_pair(v[0], v[1]), (int)bf16_pair(v[2], v[3]), (int)bf16_pair(v[4], v[5]), (int)bf16_pair(v[6], v[7])};
+        if (VEC) *reinterpret_cast<v4i*>(p) = q;
+        else *reinterpret_cast<v4i_at2*>(p) = q;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -119,9 +132,16 @@ __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) 
 }
 template <bool VEC>
 __device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
-    if constexpr (VEC) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    if (VEC || n >= 8) {
+        const v4f a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+        typedef v4f v4f_at4 __attribute__((aligned(4)));
+        if (VEC) {
+            reinterpret_cast<v4f*>(p)[0] = a;
+            reinterpret_cast<v4f*>(p)[1] = b;
+        } else {
+            reinterpret_cast<v4f_at4*>(p)[0] = a;
+            reinterpret_cast<v4f_at4*>(p)[1] = b;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

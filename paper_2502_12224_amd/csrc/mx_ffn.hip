@@ -12,7 +12,7 @@ fate_status launch_mx_tile(hipStream_t st, const MxArgs& a, bool up);
 long long mx_tile_items(const MxArgs& a, bool up, int RT);
 int mx_tile_rows(const MxArgs& a, bool up);
 fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x, const MxMatrix& m, const float* bias,
-                                  void* y, long long ld_y, int N, int K, int R, int y_fp32, int y_vec);
+                                  void* y, long long ld_y, int N, int K, int R, int y_fp32);
 
 struct MxCombineArgs {
     const void* rows_r; const void* rows_s;
@@ -180,15 +180,15 @@ extern "C" fate_status fate_mx_linear(void* stream, int N, int K, int R, const v
     FATE_CHECK_PTR(y);
     MxMatrix m{static_cast<const uint8_t*>(w_codes), static_cast<const uint8_t*>(w_scales), nullptr, nullptr, bits,
                mx_steps(K), mx_step_groups(K), R};
-    const int y_fp32 = y_type == FATE_FP32, y_vec = ld_y % 4 == 0;
+    const int y_fp32 = y_type == FATE_FP32;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (x_type == FATE_BF16) return launch_mx_linear_bf16(st, x, ld_x, m, bias, y, ld_y, N, K, R, y_fp32, y_vec);
+    if (x_type == FATE_BF16) return launch_mx_linear_bf16(st, x, ld_x, m, bias, y, ld_y, N, K, R, y_fp32);
     MxArgs a{};
     a.direct = m;
     a.E = 0; a.n_shared = 1; a.N = N; a.k = 1;
     a.x_s = static_cast<const uint8_t*>(x); a.xs_s = static_cast<const uint8_t*>(x_scales); a.Kp_s = mx_padded(K);
     a.y_s = y; a.ld_s = ld_y; a.cols_s = R; a.K_s = K;
-    a.down = 1; a.y_fp32 = y_fp32; a.y_vec = y_vec; a.bias = bias;
+    a.down = 1; a.y_fp32 = y_fp32; a.bias = bias;
     a.parts_r = a.parts_s = 1;
     return launch_product(st, a, false);
 }
@@ -248,7 +248,6 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     a.Kp_s = d->n_shared ? mx_padded(d->I_shared_max) : 0; a.K_s = d->I_shared_max;
     a.y_r = base + w.rows_r; a.y_s = base + w.rows_s;
     a.ld_r = a.ld_s = a.cols_r = a.cols_s = d->H;
-    a.y_vec = 1;
     a.parts_r = a.parts_s = 1;
     a.part_r = (long long)d->N * d->k * d->H;
     a.part_s = (long long)d->N * d->n_shared * d->H;

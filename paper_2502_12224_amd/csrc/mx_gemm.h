@@ -32,7 +32,7 @@ struct MxArgs {
     int parts_r, parts_s;
     long long part_r, part_s;
     int down;                               // entries' w2 with K = I; otherwise w1 (and w3) with K = H
-    int y_fp32, y_vec;                      // output type; rows allow 4-wide stores
+    int y_fp32;                             // output type
     const float* bias;
     int32_t* status;
 };
@@ -249,17 +249,20 @@ __device__ __forceinline__ void mx_store_h(const v4f& h0, const v4f& h1, bool li
     }
 }
 
-// Four consecutive outputs of one row.
-__device__ __forceinline__ void mx_store_y(bool y_fp32, bool y_vec, void* y, long long at, int left, v4f v) {
+// Four consecutive outputs of one row, of which the first `left` exist; wherever they lie.
+__device__ __forceinline__ void mx_store_y(bool y_fp32, void* y, long long at, int left, v4f v) {
+    typedef v4f v4f_at4 __attribute__((aligned(4)));
+    typedef long long pair_at2 __attribute__((aligned(2)));
     if (y_fp32) {
         float* p = static_cast<float*>(y) + at;
-        if (y_vec && left >= 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        if (left >= 4) *reinterpret_cast<v4f_at4*>(p) = v;
         else
             for (int i = 0; i < 4; ++i)
                 if (i < left) p[i] = v[i];
     } else {
         uint16_t* p = static_cast<uint16_t*>(y) + at;
-        if (y_vec && left >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        if (left >= 4)
+            *reinterpret_cast<pair_at2*>(p) = (long long)((unsigned long long)bf16_pair(v[2], v[3]) << 32 | bf16_pair(v[0], v[1]));
         else
             for (int i = 0; i < 4; ++i)
                 if (i < left) p[i] = (uint16_t)f32_to_bf16_bits(v[i]);

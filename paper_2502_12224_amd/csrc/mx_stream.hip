@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kStreamThreads, 4) void mx_stream_kernel(MxArgs a, 
     const int tile = wave / KS, ks = wave % KS;
     const long long out0 = shared ? (long long)(it.group - a.E) * a.N + it.row0 : it.row0;   // first output row
     const MxSide sd = mx_side(a, shared);
-    const bool y_fp32 = a.y_fp32, y_vec = a.y_vec;
+    const bool y_fp32 = a.y_fp32;
     MxRowStage rows;
     rows.Kp = sd.Kp;
     rows.x = sd.x;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kStreamThreads, 4) void mx_stream_kernel(MxArgs a, 
         if (!UP && ks == 0 && (lane & 15) < it.rows) {
             const int r0 = (it.col * NT + tile) * 16 + 4 * g;
             if (r0 < sd.cols)
-                mx_store_y(y_fp32, y_vec, sd.y, (out0 + (lane & 15)) * sd.ld + r0, sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
+                mx_store_y(y_fp32, sd.y, (out0 + (lane & 15)) * sd.ld + r0, sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
         }
         return;
     }
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kStreamThreads, 4) void mx_stream_kernel(MxArgs a, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i] += r0 + i < sd.cols ? ld_global<float>(a.bias, r0 + i) : 0.0f;
             }
-            mx_store_y(y_fp32, y_vec, sd.y, (out0 + (lane & 15)) * sd.ld + r0, sd.cols - r0, acc);
+            mx_store_y(y_fp32, sd.y, (out0 + (lane & 15)) * sd.ld + r0, sd.cols - r0, acc);
         }
     }
 }
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(64 * kOneWaves) void mx_down_one_kernel(MxOneArgs o
         v4f y = red[threadIdx.x];
         for (int w = 1; w < kOneWaves; ++w) y += red[w * 4 + threadIdx.x];
         const int r0 = (int)blockIdx.x * 16 + 4 * (int)threadIdx.x;
-        mx_store_y(o.y_fp32, true, o.y, r0, o.H - r0, y);
+        mx_store_y(o.y_fp32, o.y, r0, o.H - r0, y);
     }
 }
 
@@ -385,7 +385,7 @@ struct MxBf16Args {
     MxMatrix m;
     const float* bias;
     void* y; long long ld_y;
-    int N, K, R, y_fp32, y_vec, x_vec;
+    int N, K, R, y_fp32, x_vec;
     int rows_cap, passes;               // tokens per pass
 };
 
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
         const int r = q / per_row, i = (q - r * per_row) * 8;
         const uint16_t* src = a.x + (t0 + r) * a.ld_x + i;
         v4i v = {0, 0, 0, 0};
-        if (a.x_vec && i + 8 <= a.K) v = ld_global<v4i>(src);
+        if (i + 8 <= a.K) v = a.x_vec ? ld_global<v4i>(src) : (v4i)ld_global<v4i_at2>(src);
         else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += r0 + i < a.R ? a.bias[r0 + i] : 0.0f;
         }
-        mx_store_y(a.y_fp32, a.y_vec, a.y, (t0 + (lane & 15)) * a.ld_y + r0, a.R - r0, acc);
+        mx_store_y(a.y_fp32, a.y, (t0 + (lane & 15)) * a.ld_y + r0, a.R - r0, acc);
     }
 }
 
@@ -573,10 +573,10 @@ fate_status launch_mx_down_one(hipStream_t st, const MxArgs& a, const float* top
 }
 
 fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x, const MxMatrix& m, const float* bias,
-                                  void* y, long long ld_y, int N, int K, int R, int y_fp32, int y_vec) {
+                                  void* y, long long ld_y, int N, int K, int R, int y_fp32) {
     MxBf16Args a{};
     a.x = static_cast<const uint16_t*>(x); a.ld_x = ld_x; a.m = m; a.bias = bias; a.y = y; a.ld_y = ld_y;
-    a.N = N; a.K = K; a.R = R; a.y_fp32 = y_fp32; a.y_vec = y_vec;
+    a.N = N; a.K = K; a.R = R; a.y_fp32 = y_fp32;
     a.x_vec = ld_x % 8 == 0;
     const int row_bytes = (m.KT * kMxStep + 8) * 2;
     a.rows_cap = (kMaxLds - kRedBytes) / row_bytes;

@@ -146,7 +146,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, int
         }
     } else {
         const int cols = sd.cols;
-        const bool y_fp32 = a.y_fp32, y_vec = a.y_vec;
+        const bool y_fp32 = a.y_fp32;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int r = t * 16 + (lane & 15);
@@ -160,7 +160,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, int
 #pragma unroll
                             for (int b = 0; b < 4; ++b) v[b] += r0 + b < cols ? ld_global<float>(a.bias, r0 + b) : 0.0f;
                         }
-                        mx_store_y(y_fp32, y_vec, sd.y, part * sd.part + (out0 + r) * ld + r0, cols - r0, v);
+                        mx_store_y(y_fp32, sd.y, part * sd.part + (out0 + r) * ld + r0, cols - r0, v);
                     }
                 }
             }
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256, RT >= 128 ? 2 : 3) void mx_tile_kernel(MxArgs 
             for (int q = (int)threadIdx.x; q < it.rows * 64; q += 256) {
                 const int r = q >> 6, r0 = it.col * 256 + (q & 63) * 4;
                 if (r0 < sd.cols)
-                    mx_store_y(a.y_fp32, a.y_vec, sd.y, part * sd.part + (out0 + r) * sd.ld + r0,
+                    mx_store_y(a.y_fp32, sd.y, part * sd.part + (out0 + r) * sd.ld + r0,
                                sd.cols - r0, v4f{0.0f, 0.0f, 0.0f, 0.0f});
             }
         }
