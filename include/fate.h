@@ -416,8 +416,7 @@ fate_status fate_mx_linear(void* stream, int N, int K, int R, const void* x, int
  * multiples of 32, mode 0.  An activated expert with a NULL matrix or scale is
  * flagged in the int32 at workspace offset 0 (bit 0; the caller clears it) and
  * contributes nothing, as does (bit 2) an entry of another format.  Sums as in fate_mx_linear; the rows of the down
- * product (of long reductions: of parts of it) are kept in fp32, or, for more than
- * a few tokens, in y's type until they are added up in fp32.
+ * product (of long reductions: of parts of it) are kept and added up in fp32.
  * workspace: what calls of up to N tokens need; calls that share one are ordered
  * on one stream.
  * ---------------------------------------------------------------------- */

@@ -15,7 +15,7 @@ fate_status launch_mx_linear_bf16(hipStream_t st, const void* x, long long ld_x,
                                   void* y, long long ld_y, int N, int K, int R, int y_fp32);
 
 struct MxCombineArgs {
-    const void* rows_r; const void* rows_s;
+    const float* rows_r; const float* rows_s;
     const int32_t* inv_perm; const float* topk_w;
     const uint8_t* x; const uint8_t* xs; const uint16_t* gate;
     void* y;
@@ -25,17 +25,16 @@ struct MxCombineArgs {
 };
 
 // Eight consecutive columns of a row, times w, onto y.
-template <typename T>
-__device__ __forceinline__ void add_row8(const void* rows, long long at, float w, float (&y)[8]) {
+__device__ __forceinline__ void add_row8(const float* rows, long long at, float w, float (&y)[8]) {
     float v[8];
-    load8<true>(static_cast<const T*>(rows) + at, 8, v);
+    load8<true>(rows + at, 8, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = fmaf(w, v[i], y[i]);
 }
 
 // y[t] = sum_j w[t,j] row[inv_perm[t,j]] + g(t) sum_v shared row: one workgroup per token, terms in the order of j, then v.
 // Few tokens: two round trips and the launch (the rows are requested before the gate is known); many: memory.
-template <typename T, typename TY>
+template <typename TY>
 __global__ __launch_bounds__(512) void mx_combine_kernel(MxCombineArgs a) {
     __shared__ float part[8];
     const long long t = blockIdx.x;
@@ -69,11 +68,11 @@ __global__ __launch_bounds__(512) void mx_combine_kernel(MxCombineArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (j0 + j < a.k && (unsigned)s[j] < (unsigned)P)
-                        for (int p = 0; p < a.parts_r; ++p) add_row8<T>(a.rows_r, p * a.part_r + (long long)s[j] * a.H + i, w[j], y);
+                        for (int p = 0; p < a.parts_r; ++p) add_row8(a.rows_r, p * a.part_r + (long long)s[j] * a.H + i, w[j], y);
             }
             for (int v = 0; v < a.n_shared * a.parts_s; ++v) {
                 const int p = v / a.n_shared;
-                add_row8<T>(a.rows_s, p * a.part_s + ((long long)(v - p * a.n_shared) * a.N + t) * a.H + i, 1.0f, z);
+                add_row8(a.rows_s, p * a.part_s + ((long long)(v - p * a.n_shared) * a.N + t) * a.H + i, 1.0f, z);
             }
         }
         if (a.gate != nullptr && i0 == 0) {
@@ -115,7 +114,13 @@ static fate_status check_mx_desc(const fate_ffn_desc* d) {
     return FATE_OK;
 }
 
-constexpr int kMxMostParts = 4;
+// A shared expert's reduction may be several times as long as a routed one's: parts of about that length (Qwen shape, 4
+// parts: 512 tokens 126 -> 107 us, 2048 tokens 276 -> 228).
+static int mx_shared_parts(const fate_ffn_desc& d) {
+    const int kr = mx_steps(d.I_max), ks = d.n_shared ? mx_steps(d.I_shared_max) : 0;
+    const int parts = ks > kr ? (ks + kr / 2) / kr : 1;
+    return parts < 4 ? parts : 4;
+}
 
 struct MxWorkspace {
     size_t h_r, hs_r, h_s, hs_s, rows_r, rows_s, bytes;
@@ -131,10 +136,11 @@ static MxWorkspace mx_workspace(const fate_ffn_desc& d) {
     w.hs_r = off; off += up(P * Ip / kMxBlock);
     w.h_s = off; off += up(S * Is);
     w.hs_s = off; off += up(S * Is / kMxBlock);
-    // (room for two parts of routed rows and the most of shared ones, in bf16 more than one part in fp32: what calls of
-    // up to N tokens need rises with N)
-    w.rows_r = off; off += up(P * d.H * (d.y_is_fp32 ? 4 : 2) * 2);
-    w.rows_s = off; off += up(S * d.H * (d.y_is_fp32 ? 4 : 2) * kMxMostParts);
+    // fp32: the rows, and their parts all the more, are terms of the token's sum (in bf16 the output's error against 64
+    // bits rises from 1.7e-3, its own rounding, to 2.6e-3).  (room for two parts of routed rows whatever N: what calls
+    // of up to N tokens need rises with N)
+    w.rows_r = off; off += up(P * d.H * 4 * 2);
+    w.rows_s = off; off += up(S * d.H * 4 * mx_shared_parts(d));
     w.bytes = off;
     return w;
 }
@@ -256,27 +262,21 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     if (mx_one_token(a, &lds))
         return launch_mx_down_one(st, a, topk_w, static_cast<const uint8_t*>(x_codes), static_cast<const uint8_t*>(x_scales),
                                   gate, y, d->H, d->y_is_fp32);
-    const bool streamed = stream_rows(a, false) != 0;
-    a.y_fp32 = d->y_is_fp32 || streamed;                          // (few rows: their bytes do not count)
-    if (!streamed) {
-        // a shared expert's reduction may be several times as long as a routed one's: parts of about that length
-        // (Qwen shape, 4 parts: 512 tokens 126 -> 107 us, 2048 tokens 276 -> 228)
-        const int kr = mx_steps(d->I_max), ks = d->n_shared ? mx_steps(d->I_shared_max) : 0;
-        a.parts_s = ks > kr ? (ks + kr / 2) / kr : 1;
-        if (a.parts_s > kMxMostParts) a.parts_s = kMxMostParts;
+    a.y_fp32 = 1;
+    if (!stream_rows(a, false)) {
+        a.parts_s = mx_shared_parts(*d);
         // fewer workgroups than half the device holds: two parts (Mixtral shape, 256 tokens: 220 -> 186 us)
         if (mx_tile_items(a, false, mx_tile_rows(a, false)) <= 192 && mx_step_groups(d->I_max) >= 8) a.parts_r = 2;
     }
     s = launch_product(st, a, false);
     if (s != FATE_OK) return s;
 
-    MxCombineArgs c{base + w.rows_r, base + w.rows_s, inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
+    MxCombineArgs c{static_cast<const float*>(a.y_r), static_cast<const float*>(a.y_s), inv_perm, topk_w, static_cast<const uint8_t*>(x_codes),
                     static_cast<const uint8_t*>(x_scales), gate,
                     y, d->N, d->k, d->H, d->n_shared, mx_padded(d->H), a.parts_r, a.parts_s, a.part_r, a.part_s};
     const int threads = d->H >= 4096 ? 512 : (d->H + 511) / 512 * 64;
-    if (d->y_is_fp32) mx_combine_kernel<float, float><<<d->N, threads, 0, st>>>(c);
-    else if (a.y_fp32) mx_combine_kernel<float, uint16_t><<<d->N, threads, 0, st>>>(c);
-    else mx_combine_kernel<uint16_t, uint16_t><<<d->N, threads, 0, st>>>(c);
+    if (d->y_is_fp32) mx_combine_kernel<float><<<d->N, threads, 0, st>>>(c);
+    else mx_combine_kernel<uint16_t><<<d->N, threads, 0, st>>>(c);
     FATE_HIP(hipGetLastError());
     return FATE_OK;
 }
