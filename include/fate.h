@@ -415,8 +415,10 @@ fate_status fate_mx_linear(void* stream, int N, int K, int R, const void* x, int
  * any others.  Descriptor: group and shared_group 32, H, I_max and I_shared_max
  * multiples of 32, mode 0.  An activated expert with a NULL matrix or scale is
  * flagged in the int32 at workspace offset 0 (bit 0; the caller clears it) and
- * contributes nothing, as does (bit 2) an entry of another format.  Sums as in fate_mx_linear; the rows of the down
- * product (of long reductions: of parts of it) are kept and added up in fp32.
+ * contributes nothing, as does (bit 2) an entry of another format.  Sums as in fate_mx_linear, but
+ * with whole products where 8-bit W1 and W3 meet x (their values, codes times
+ * scale, have to lie within bf16's range); the rows of the down product (of long
+ * reductions: of parts of it) are kept and added up in fp32.
  * workspace: what calls of up to N tokens need; calls that share one are ordered
  * on one stream.
  * ---------------------------------------------------------------------- */

@@ -224,6 +224,57 @@ template <> struct MxWTile<8> {
     static constexpr int kBytes = 2048;
 };
 
+// ---- weights and rows as the bf16 numbers they are (codes have four significant bits or fewer: nothing is rounded) --
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
+template <int SEL4>
+__device__ __forceinline__ v2bf mx_pair4(uint32_t d, float s) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, s, SEL4); }
+
+// Eight of a lane's 32 weights, or of its 32 codes of a row: columns 8 j .. + 7 of its own order.
+template <int BITS>
+__device__ __forceinline__ v8bf mx_eight(const MxWTile<BITS>& t, int j, float s) {
+    v2bf p[4];
+    if constexpr (BITS == 4) {
+        const uint32_t d = (uint32_t)t.v[j];
+        p[0] = mx_pair4<0>(d, s); p[1] = mx_pair4<1>(d, s); p[2] = mx_pair4<2>(d, s); p[3] = mx_pair4<3>(d, s);
+    } else {
+        const uint32_t a = (uint32_t)t.v[2 * j], b = (uint32_t)t.v[2 * j + 1];
+        p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false);
+        p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true);
+        p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false);
+        p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
+    }
+    v8bf r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = p[i >> 1][i & 1];
+    return r;
+}
+
+// 8-bit tiles: the scale of lane l is that of block l / 16, its codes lie in blocks g / 2 (half 0) and 2 + g / 2 (g = l / 16).
+__device__ __forceinline__ float mx_half_scale(uint32_t ws, int half) {
+    const int lane = (int)(threadIdx.x & 63);
+    return mx_scale_f32((uint32_t)__shfl((int)ws, (lane & 15) + 16 * (lane >> 5) + 32 * half) & 255u);
+}
+
+// mx_mfma8 with every product whole.  The 8-bit instruction cuts the products of eight consecutive columns at 2^-15 of the
+// largest, 1.5e-5 of the sum as a rule; the four instructions for bf16 take twice its cycles.  That
+// is worth it where the sum is rounded to a code afterwards, since some values then round the other way: an FFN of 64
+// experts and two 8-bit shared ones has, in bf16 and against 64 bits, an error of 1.65e-3 to 1.68e-3 by seed (the output's
+// own rounding), with the 8-bit instruction of 1.7e-3 to 3.2e-3.  Its time, 8-bit instruction / this one: 8 tokens
+// 50 / 50 us, 64 tokens 83 / 85, 256 tokens 102 / 125, 1024 tokens 156 / 237.  (4-bit weights: 1.6e-3 to 2.1e-3 as it is.)
+// x0, x1: scale bytes of the row's blocks g / 2 and 2 + g / 2.
+__device__ __forceinline__ v4f mx_mfma8_exact(const MxWTile<8>& w, uint32_t ws, v8i x, uint32_t x0, uint32_t x1, v4f acc) {
+    const float f0 = mx_half_scale(ws, 0), f1 = mx_half_scale(ws, 1);
+    const float e0 = mx_scale_f32(x0), e1 = mx_scale_f32(x1);
+    const MxWTile<8> xt{x};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_eight<8>(w, i, i < 2 ? f0 : f1), mx_eight<8>(xt, i, i < 2 ? e0 : e1), acc, 0, 0, 0);
+    return acc;
+}
+
 __device__ __forceinline__ float mx_swiglu(float a, float b) { return a / (1.0f + __expf(-a)) * b; }
 
 // 32 neurons of 16 tokens after the up product (two tiles of 16 neurons, four per lane in each) -> codes and scale of

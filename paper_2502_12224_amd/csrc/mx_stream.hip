@@ -55,8 +55,8 @@ struct MxRowStage {
 };
 
 // The wave's tiles s0 .. s1 - 1 of one tile row, multiplied with the rows in LDS; rows behind the last one read row 0
-// (their sums are not stored).
-template <int BITS>
+// (their sums are not stored).  EXACT: see mx_mfma8_exact.
+template <int BITS, bool EXACT>
 __device__ __forceinline__ v4f stream_tiles(const uint8_t* w, const uint8_t* ws, int s0, int s1, MxRowStage& rows,
                                             uint8_t* xl, uint8_t* sl) {
     constexpr int R = kStreamRing<BITS>;
@@ -85,7 +85,11 @@ __device__ __forceinline__ v4f stream_tiles(const uint8_t* w, const uint8_t* ws,
                 const v4i lo = *reinterpret_cast<const v4i*>(xr + s * kMxStep);
                 const v4i hi = *reinterpret_cast<const v4i*>(xr + s * kMxStep + 64);
                 const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                acc = wt[j].template mfma<0>(sc[j] >> (8 * (s & 3)), x, sr[s * 4], acc);
+                const uint32_t d = sc[j] >> (8 * (s & 3));
+                if constexpr (EXACT && BITS == 8) {
+                    const uint8_t* e = sr - g + s * 4 + (g >> 1);
+                    acc = mx_mfma8_exact(wt[j], d, x, e[0], e[2], acc);
+                } else acc = wt[j].template mfma<0>(d, x, sr[s * 4], acc);
             }
             if (more) {
                 const int t = s + R < end ? s + R : end;
@@ -146,8 +150,8 @@ __global__ __launch_bounds__(kStreamThreads, 4) void mx_stream_kernel(MxArgs a, 
     const uint8_t* ws = (third ? m.s3 : m.s) + (long long)rb * m.KG * 256;
     const int s0 = m.KT * ks / KS, s1 = m.KT * (ks + 1) / KS;
     v4f acc;
-    if (m.bits == 4) acc = stream_tiles<4>(w, ws, s0, s1, rows, xl, sl);
-    else acc = stream_tiles<8>(w, ws, s0, s1, rows, xl, sl);
+    if (m.bits == 4) acc = stream_tiles<4, false>(w, ws, s0, s1, rows, xl, sl);
+    else acc = stream_tiles<8, UP>(w, ws, s0, s1, rows, xl, sl);
     if constexpr (KS > 1 || UP) {
         red[wave * 64 + lane] = acc;
         __syncthreads();
@@ -354,32 +358,6 @@ __global__ __launch_bounds__(64 * kOneWaves) void mx_down_one_kernel(MxOneArgs o
 
 // ---- bf16 rows: weights become the bf16 numbers they are ----------------------------------------------------------
 
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-
-template <int SEL4>
-__device__ __forceinline__ v2bf mx_pair4(uint32_t d, float s) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, s, SEL4); }
-
-// Eight of a lane's 32 weights: columns 8 j .. + 7 of its own order.
-template <int BITS>
-__device__ __forceinline__ v8bf mx_eight(const MxWTile<BITS>& t, int j, float s) {
-    v2bf p[4];
-    if constexpr (BITS == 4) {
-        const uint32_t d = (uint32_t)t.v[j];
-        p[0] = mx_pair4<0>(d, s); p[1] = mx_pair4<1>(d, s); p[2] = mx_pair4<2>(d, s); p[3] = mx_pair4<3>(d, s);
-    } else {
-        const uint32_t a = (uint32_t)t.v[2 * j], b = (uint32_t)t.v[2 * j + 1];
-        p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false);
-        p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true);
-        p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false);
-        p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
-    }
-    v8bf r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = p[i >> 1][i & 1];
-    return r;
-}
-
 struct MxBf16Args {
     const uint16_t* x; long long ld_x;
     MxMatrix m;
@@ -460,13 +438,8 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx_linear_bf16_kernel(MxBf1
                 if (s < s1) {
                     // the lane's codes all belong to one row; 8-bit ones to two blocks of it
                     const uint32_t d = sc[j] >> (8 * (s & 3));
-                    float f0, f1;
-                    if constexpr (BITS == 4) f0 = f1 = mx_scale_f32(d & 255u);
-                    else {
-                        // scale of lane l is that of block l / 16; pieces 16 g and 64 + 16 g lie in blocks g / 2 and 2 + g / 2
-                        f0 = mx_scale_f32((uint32_t)__shfl((int)d, (lane & 15) + 16 * (g >> 1)) & 255u);
-                        f1 = mx_scale_f32((uint32_t)__shfl((int)d, (lane & 15) + 16 * (2 + (g >> 1))) & 255u);
-                    }
+                    const float f0 = BITS == 4 ? mx_scale_f32(d & 255u) : mx_half_scale(d, 0);
+                    const float f1 = BITS == 4 ? f0 : mx_half_scale(d, 1);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int off = BITS == 4 ? 8 * i : 64 * (i >> 1) + 8 * (i & 1);

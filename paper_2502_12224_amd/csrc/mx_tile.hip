@@ -106,14 +106,34 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, int
             if (s < KT) {
                 const uint8_t* xs = xr + (j & 1) * (RT * kMxStep);
                 const uint8_t* ss = sr + (j & 1) * (RT * 4);
+                if constexpr (UP && BITS == 8) {                  // (every product whole: see mx_mfma8_exact)
+                    const uint8_t* se = ss - g + (g >> 1);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const v4i lo = *reinterpret_cast<const v4i*>(xs + t * 16 * kMxStep + c0);
-                    const v4i hi = *reinterpret_cast<const v4i*>(xs + t * 16 * kMxStep + c1);
-                    const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    const uint32_t e = ss[t * 64];
+                    for (int q = 0; q < 4; ++q) {
+                        v8bf wq[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][i] = wt[j % D][i].template mfma<j>(sc[i], x, e, acc[t][i]);
+                        for (int i = 0; i < 4; ++i) wq[i] = mx_eight<8>(wt[j % D][i], q, mx_half_scale(sc[i] >> (8 * j), q >> 1));
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const uint2 v = *reinterpret_cast<const uint2*>(xs + t * 16 * kMxStep + (q < 2 ? c0 : c1) + 8 * (q & 1));
+                            const MxWTile<8> xt{v8i{(int)v.x, (int)v.y, 0, 0, 0, 0, 0, 0}};
+                            const v8bf x = mx_eight<8>(xt, 0, mx_scale_f32(se[t * 64 + 2 * (q >> 1)]));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wq[i], x, acc[t][i], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);       // (all conversions at once would spill)
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                } else {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const v4i lo = *reinterpret_cast<const v4i*>(xs + t * 16 * kMxStep + c0);
+                        const v4i hi = *reinterpret_cast<const v4i*>(xs + t * 16 * kMxStep + c1);
+                        const v8i x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        const uint32_t e = ss[t * 64];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][i] = wt[j % D][i].template mfma<j>(sc[i], x, e, acc[t][i]);
+                    }
                 }
             }
 #pragma unroll
