@@ -115,7 +115,7 @@ static fate_status check_mx_desc(const fate_ffn_desc* d) {
 }
 
 // A shared expert's reduction may be several times as long as a routed one's: parts of about that length (Qwen shape, 4
-// parts: 512 tokens 126 -> 107 us, 2048 tokens 276 -> 228).
+// parts: 512 tokens 124 -> 106 us, 2048 tokens 279 -> 233).
 static int mx_shared_parts(const fate_ffn_desc& d) {
     const int kr = mx_steps(d.I_max), ks = d.n_shared ? mx_steps(d.I_shared_max) : 0;
     const int parts = ks > kr ? (ks + kr / 2) / kr : 1;
@@ -265,7 +265,7 @@ extern "C" fate_status fate_moe_ffn_mx(void* stream, const fate_ffn_desc* d, con
     a.y_fp32 = 1;
     if (!stream_rows(a, false)) {
         a.parts_s = mx_shared_parts(*d);
-        // fewer workgroups than half the device holds: two parts (Mixtral shape, 256 tokens: 220 -> 186 us)
+        // fewer workgroups than half the device holds: two parts (Mixtral shape, 256 tokens: 220 -> 187 us)
         if (mx_tile_items(a, false, mx_tile_rows(a, false)) <= 192 && mx_step_groups(d->I_max) >= 8) a.parts_r = 2;
     }
     s = launch_product(st, a, false);

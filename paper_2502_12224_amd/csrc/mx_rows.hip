@@ -24,6 +24,7 @@ struct NormArgs {
     long long ld_h, ld_delta, ld_h_out, ld_x;
     int N, H, weight_fp32;
     float eps;
+    double inv_H;
 };
 
 // One row per 64 * W threads (W == 1: four rows per workgroup, no barrier); a thread keeps C pieces of eight elements in
@@ -67,7 +68,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_rmsnorm_kernel(Norm
 #pragma unroll
         for (int w = 0; w < W; ++w) q += part[w];
     }
-    const float r = 1.0f / sqrtf(q / (float)a.H + a.eps);
+    // r + rl = 1 / sqrt(mean + eps) to about 2^-45: the rounding of r alone turns a few values, and now and then the scale
+    // of a block, to another code (16384 x 4096: 8-bit rows off by 5.8e-5 to 6.3e-4 by seed, so by 5.1e-5 to 7.3e-5).
+    const double m = fma((double)q, a.inv_H, (double)a.eps);
+    const float r = 1.0f / sqrtf((float)m);
+    const float e = (float)fma(-m * (double)r, (double)r, 1.0);
+    const float rl = fabsf(e) < 1e-5f ? 0.5f * e * r : 0.0f;         // (a row of zeros without eps, infinities: r is)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int i = (c * T + t) * 8;
@@ -75,7 +81,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_rmsnorm_kernel(Norm
         if (n > 0 && a.h_out != nullptr) store8<VEC>(static_cast<TH*>(a.h_out) + row * a.ld_h_out + i, n, s[c]);
         float x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = s[c][j] * r;
+        for (int j = 0; j < 8; ++j) x[j] = fmaf(s[c][j], r, s[c][j] * rl);
         if (a.weight != nullptr && n > 0) {
             float w[8];
             if (a.weight_fp32) load8<VEC>(static_cast<const float*>(a.weight) + i, n, w);
@@ -209,7 +215,7 @@ extern "C" fate_status fate_add_rmsnorm(void* stream, int N, int H, const void* 
     if (h_out == h && ld_h_out != ld_h) FATE_FAIL(FATE_EINVAL, "h_out is h with another distance between rows");
     NormArgs a{h, delta, weight, h_out, static_cast<uint16_t*>(x_bf16), static_cast<uint8_t*>(x_codes),
                static_cast<uint8_t*>(x_scales), ld_h, delta ? ld_delta : 0, ld_h_out, ld_x, N, H,
-               weight_type == FATE_FP32, eps};
+               weight_type == FATE_FP32, eps, 1.0 / (double)H};
     const bool vec = H % 8 == 0 && rows_of_16_bytes(h_type, ld_h) && (!delta || rows_of_16_bytes(delta_type, ld_delta)) &&
                      (!h_out || rows_of_16_bytes(h_type, ld_h_out)) && (!x_bf16 || rows_of_16_bytes(FATE_BF16, ld_x));
     hipStream_t st = static_cast<hipStream_t>(stream);
