@@ -520,7 +520,11 @@ def fate_moe_ffn_mx(desc, x_codes, x_scales, experts_dev, counts, offsets, perm,
     if offsets.numel() <= E or perm.numel() < P or inv_perm.numel() < P or topk_w.numel() < P or \
             experts_dev.nbytes < E * 96 or (desc.n_shared and (shared_dev is None or shared_dev.nbytes < desc.n_shared * 96)):
         _refuse("a routing output or an expert table is smaller than the descriptor says")
-    if shared_gate is not None and (shared_gate.dtype != torch.bfloat16 or shared_gate.numel() < H):
+    for t in (counts, offsets, perm, inv_perm, expert_order, topk_w):
+        if not t.is_contiguous():
+            _refuse("the routing outputs and topk_w are contiguous")
+    if shared_gate is not None and (shared_gate.dtype != torch.bfloat16 or shared_gate.numel() < H or
+                                    not shared_gate.is_contiguous()):
         _refuse("shared_gate is a bf16 vector [H]")
     _check(lib().fate_moe_ffn_mx(_here(stream, x_codes, x_scales, experts_dev, counts, offsets, perm, inv_perm,
                                        expert_order, topk_w, shared_dev, shared_gate, y, workspace), C.addressof(desc),

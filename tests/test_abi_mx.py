@@ -114,3 +114,24 @@ def test_binding_refusals():
     for f in bad:
         with pytest.raises(B.FateError):
             f()
+
+
+def test_ffn_binding_refusals():
+    N, H, E, k = 3, 128, 4, 2
+    d = B.make_ffn_desc(N, H, E, k, 64, 4, 32, 0, 0, 4, 32, True)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    good = dict(x=B.mx_empty(N, H, device="cpu"), table=torch.zeros(E * 96, dtype=torch.uint8), counts=i32(E), offsets=i32(E + 1),
+                perm=i32(N * k), inv=i32(N * k), order=i32(E), w=torch.zeros(N, k), gate=None, y=torch.zeros(N, H))
+
+    def call(**kw):
+        a = dict(good, **kw)
+        B.fate_moe_ffn_mx(d, *a["x"], a["table"], a["counts"], a["offsets"], a["perm"], a["inv"], a["order"], a["w"], None, a["gate"],
+                          a["y"], torch.zeros(1 << 20, dtype=torch.uint8))
+    bad = [dict(w=torch.zeros(N, 2 * k)[:, ::2]), dict(w=torch.zeros(N, k + 1)[:, :k]), dict(perm=i32(2 * N * k)[::2]),
+           dict(counts=i32(2 * E)[::2]), dict(perm=i32(N * k - 1)), dict(offsets=i32(E)), dict(w=torch.zeros(N, k).half()),
+           dict(inv=i32(N * k).long()), dict(table=torch.zeros(E * 96 - 1, dtype=torch.uint8)), dict(y=torch.zeros(N, H).t()),
+           dict(y=torch.zeros(N, H).bfloat16()), dict(x=B.mx_empty(N + 1, H, device="cpu")),
+           dict(gate=torch.zeros(2 * H, dtype=torch.bfloat16)[::2]), dict(gate=torch.zeros(H))]
+    for kw in bad:
+        with pytest.raises(B.FateError):
+            call(**kw)
