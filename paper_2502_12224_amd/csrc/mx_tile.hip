@@ -19,8 +19,11 @@ template <int RT, bool UP, int BITS>
 __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, int part, const MxMatrix& m, uint8_t* lds) {
     constexpr int NT = RT / 16;                                   // row tiles of 16
     constexpr int NL = RT >= 32 ? RT / 32 : 1;                    // pieces of 16 bytes of the rows per thread and step
-    constexpr int D = BITS == 8 ? (RT >= 128 ? 2 : 1) : RT >= 64 ? 2 : 4;   // weight tiles in flight per tile row
-    constexpr int XD = RT >= 128 ? 1 : 2;                         // steps of rows in registers (128: 256 registers are full)
+    // Whole products of 8-bit codes need registers for the bf16 numbers: more steps in flight would spill (two steps of
+    // weights, 128 rows: 1024 tokens 237 us, one 211; two of rows, 64 rows: 256 tokens 125 us, one 115).
+    constexpr bool whole = UP && BITS == 8;
+    constexpr int D = BITS == 8 ? (RT >= 128 && !whole ? 2 : 1) : RT >= 64 ? 2 : 4;     // weight tiles in flight per tile row
+    constexpr int XD = RT >= 128 || (RT >= 64 && whole) ? 1 : 2;  // steps of rows in registers (128: 256 registers are full)
     const int lane = (int)(threadIdx.x & 63), g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const bool shared = it.group >= a.E;
     const MxSide sd = mx_side(a, shared);
@@ -106,7 +109,7 @@ __device__ __forceinline__ void tile_body(const MxArgs& a, const MxItem& it, int
             if (s < KT) {
                 const uint8_t* xs = xr + (j & 1) * (RT * kMxStep);
                 const uint8_t* ss = sr + (j & 1) * (RT * 4);
-                if constexpr (UP && BITS == 8) {                  // (every product whole: see mx_mfma8_exact)
+                if constexpr (whole) {                            // (as mx_mfma8_exact)
                     const uint8_t* se = ss - g + (g >> 1);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
